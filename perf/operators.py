@@ -434,9 +434,11 @@ def _own(s):
                                      workspace=s["ws"]))
         return m3.ffn_bwd(s["x"], s["Wg"], s["Wu"], s["Wd"], s["dy"], act=s["act"],
                           workspace=s["ws"])
-    m3.adamw_step(s["p"], s["g"], s["m"], s["v"], step=s["step"], lr=s["lr"], betas=s["betas"],
-                  eps=s["eps"], weight_decay=s["wd"], grad_scale=s["grad_scale"],
-                  low=s.get("low"), scales=s.get("scales"), seed=s["seed"])
+    if "table" not in s:   # a program builds its table once and keeps it
+        s["table"] = m3.adamw_table(s["p"], s["g"], s["m"], s["v"], weight_decay=s["wd"],
+                                    low=s.get("low"), scales=s.get("scales"))
+    m3.adamw_step(s["table"], step=s["step"], lr=s["lr"], betas=s["betas"], eps=s["eps"],
+                  grad_scale=s["grad_scale"], seed=s["seed"])
     return s["flat"]
 
 
