@@ -479,6 +479,122 @@ m3_status m3_scan_check(const m3_dims *dims, const void *workspace, size_t works
  */
 void m3_set_wait_limit(uint32_t polls);
 
+/*
+ * Gated linear recurrence, one decay per channel and token (the sequence
+ * mixer for layers that the scan above does not serve: its decay is one
+ * scalar per head and token).  For every batch row and channel d:
+ *
+ *     rho_t = sigmoid(r_t),  iota_t = sigmoid(i_t),  log a_t = A_d rho_t
+ *     h_t = a_t h_{t-1} + sqrt(1 - a_t^2) iota_t x_t
+ *     y_t = h_t            (z NULL)      or      y_t = h_t SiLU(z_t)
+ *
+ * with h_{-1} = init_state (NULL: zero) and final_state = h_{L-1}.  A is the
+ * log-decay of an open gate, fp32 [width], <= 0 (A > 0 gives NaN).
+ * x, r, i and z are [batch][seqlen][width] in the io dtype with any strides of
+ * batch and token (elements, in m3_glr_dims) and a channel stride of 1, so
+ * slices of one projection's output are taken as they are; y is contiguous.
+ * States are fp32 [batch][width].  Inputs of a token reach no earlier token;
+ * a non-finite one spoils the later tokens of its channel.
+ *
+ * m3_glr_fwd: y and final_state, and with `states` not NULL the state that
+ * enters each run of M3_GLR_CHUNK tokens, [batch][ceil(seqlen /
+ * M3_GLR_CHUNK)][width] fp32, which m3_glr_bwd takes.  One launch: runs of
+ * tokens go to workgroups that find the state entering theirs by a bounded
+ * look-back (m3_glr_check and m3_set_wait_limit as for the scans; a wait that
+ * gave up leaves NaN).  seqlen 0 passes the state through (x, r, i, z, y may
+ * be NULL).
+ *
+ * m3_glr_bwd: gradients of J given dy = dJ/dy (contiguous, io dtype) and
+ * dfinal = dJ/dfinal_state (NULL: zero), from the forward's inputs and
+ * `states`: dx, dr, di and, with z, dz (contiguous, io dtype), dA [width]
+ * (summed over batch and tokens in fp64 from fp32 parts), and with
+ * dinit_state not NULL the initial state's, [batch][width].  Everything is
+ * overwritten.  Where a_t rounds to 1 the derivative of sqrt(1 - a_t^2) has
+ * no finite value; its products in dr and dA tend to zero and are taken so.
+ *
+ * m3_glr_step: one token; x, r, i and z [batch][width] (batch strides; the
+ * token strides and seqlen are ignored), state updated in place, y
+ * [batch][width] contiguous.
+ *
+ * Workspace: m3_glr_workspace_bytes(dims) bytes serve both calls (0 on
+ * invalid dims).  It must be zero-filled before its first use and then be
+ * used by m3_glr_* calls only, of any dims, one at a time.  Deterministic.
+ * Alignment: the workspace 16 bytes, everything else its element's (else
+ * M3_ERR_ALIGN); in bf16 two channels are moved at a time where the width, the
+ * strides and the token arrays' addresses are even in elements.  Outputs must
+ * not overlap inputs.
+ */
+#define M3_GLR_CHUNK 128
+typedef struct {
+    int64_t batch;      /* >= 1                                              */
+    int64_t seqlen;     /* >= 0 (ignored by m3_glr_step)                     */
+    int64_t width;      /* channels, >= 1                                    */
+    int32_t io;         /* m3_dtype of x, r, i, z, y and their gradients     */
+    int32_t flags;      /* must be 0                                         */
+    int64_t x_stride_b, x_stride_t, r_stride_b, r_stride_t; /* in elements,  */
+    int64_t i_stride_b, i_stride_t, z_stride_b, z_stride_t; /* >= 0          */
+} m3_glr_dims;
+size_t m3_glr_workspace_bytes(const m3_glr_dims *dims);
+m3_status m3_glr_fwd(const m3_glr_dims *dims, const void *x, const void *r, const void *i,
+                     const float *A, const void *z, const float *init_state, void *y,
+                     float *final_state, float *states, void *workspace, size_t workspace_bytes,
+                     void *stream);
+m3_status m3_glr_bwd(const m3_glr_dims *dims, const void *x, const void *r, const void *i,
+                     const float *A, const void *z, const float *states, const void *dy,
+                     const float *dfinal, void *dx, void *dr, void *di, void *dz, float *dA,
+                     float *dinit_state, void *workspace, size_t workspace_bytes, void *stream);
+m3_status m3_glr_step(const m3_glr_dims *dims, float *state, const void *x, const void *r,
+                      const void *i, const float *A, const void *z, void *y, void *stream);
+m3_status m3_glr_check(const m3_glr_dims *dims, const void *workspace, size_t workspace_bytes,
+                       uint32_t *timeouts, void *stream);
+
+/*
+ * AdamW over many tensors (decoupled weight decay), in place, one launch for
+ * every 48 tensors, nothing else on the device:
+ *
+ *     g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *     p = (1 - lr decay) p - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * p fp32, g fp32 or bf16 (grad_dtype, one for all), m and v fp32, all with n
+ * elements; low (NULL: none) receives p rounded to bf16.  grad_scale is a
+ * DEVICE scalar (NULL: 1), e.g. the coefficient that clips the gradients'
+ * norm.  n = 0 is allowed.  Every operation is rounded to fp32 by itself.
+ *
+ * 8-bit states (M3_ADAMW_8BIT): m and v hold e4m3 codes (1 byte an element) of
+ * m and of sqrt(v), divided by scales[n / 256 rounded up][2] (fp32; m's, then
+ * sqrt(v)'s): each block of 256 elements has its largest magnitude / 448 as
+ * scale, 0 where all are zero.  Zero codes with any scale are the zero state.
+ * They are rounded stochastically with 16 bits each of a hash of the element's
+ * index in its tensor and the low 32 bits of (seed + the tensor's place in the
+ * call), so pass another seed for every step; a sqrt(v) that is not zero is
+ * stored as at least the smallest code.  A non-finite gradient spoils its
+ * block.
+ * Pointers need their element's alignment (else M3_ERR_ALIGN); whole vectors
+ * are moved where p, g, m, v and low are aligned for four elements.  A
+ * NULL table with count > 0, or a NULL pointer in a tensor with n > 0, is
+ * M3_ERR_NULL; n < 0, step < 1, a beta outside [0, 1), eps < 0, or a lr,
+ * decay or eps that is not finite is M3_ERR_SHAPE.
+ */
+#define M3_ADAMW_8BIT 1
+typedef struct {
+    float *p;
+    const void *g;
+    void *m, *v;
+    void *low;
+    float *scales;      /* with M3_ADAMW_8BIT, else ignored                  */
+    int64_t n;
+    double decay;       /* this tensor's weight decay                        */
+} m3_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;       /* t >= 1                                            */
+    uint64_t seed;
+    int32_t grad_dtype; /* m3_dtype of every g                               */
+    int32_t flags;      /* M3_ADAMW_8BIT or 0                                */
+} m3_adamw_config;
+m3_status m3_adamw_step(const m3_adamw_config *config, const m3_adamw_tensor *tensors,
+                        int64_t count, const float *grad_scale, void *stream);
+
 /* Static description of a status code. */
 const char *m3_status_string(m3_status status);
 

@@ -1,0 +1,37 @@
+// Kernel arguments of the AdamW step (m3_adamw.hip), already validated by the
+// front end (m3_layers.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace m3 {
+namespace adamw {
+
+constexpr int kBlockElems = 256;     // elements that share the scales of 8-bit states
+constexpr int kChunkElems = 4096;    // elements a workgroup
+constexpr int kTensors = 48;         // tensors a launch (their table is a kernel argument)
+
+struct Tensor {
+    float *p;
+    const void *g;
+    void *m, *v;
+    void *low;           // bf16 copy of p, or null
+    float *scales;       // [blocks][2], 8-bit states only
+    int64_t n;
+    float keep;          // 1 - lr * weight decay
+    uint32_t seed;
+};
+struct Args {
+    Tensor t[kTensors];
+    int32_t start[kTensors + 1];     // first workgroup of each tensor
+    int32_t count;
+    float b1, c1, b2, c2;            // beta and 1 - beta
+    float rate, root, eps;           // lr / (1 - beta1^t), (1 - beta2^t)^(-1/2)
+    const float *grad_scale;         // device scalar, or null
+};
+static_assert(sizeof(Args) <= 4096, "kernel arguments");
+
+hipError_t launch(const Args &a, bool grad_f32, bool eight, hipStream_t s);
+
+}  // namespace adamw
+}  // namespace m3

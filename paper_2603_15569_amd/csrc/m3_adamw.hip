@@ -1,0 +1,219 @@
+// AdamW over many tensors in one launch (a table of up to kTensors of them
+// goes along as a kernel argument):
+//     g' = grad_scale g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2
+//     p = (1 - lr wd) p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+// with m and v in fp32, or in 8 bits: m and sqrt(v) as e4m3 with one fp32
+// scale each for 256 elements (their largest magnitude / 448).  The 8-bit
+// states are rounded stochastically: a moving average with a decay near one
+// moves by less than a rounding step a time, and to nearest it would stand
+// still; up or down with the probabilities of the part cut off, it moves as it
+// should on average.  (sqrt(v), not v: half the range in powers of two.)  The
+// random numbers are a hash of the element's index and the tensor's seed.
+//
+// Streaming: every byte is read and written once.  A wave takes blocks of 256
+// consecutive elements, four a lane, so an 8-bit block's largest magnitude is
+// one wave reduction.  Every operation is rounded by itself (no contraction).
+#include "m3_adamw.h"
+#include "m3_device.h"
+
+namespace m3 {
+namespace adamw {
+namespace {
+
+constexpr int kWaves = 4, kPer = kChunkElems / (kWaves * kBlockElems);   // blocks a wave
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
+    return v;
+}
+__device__ __forceinline__ uint32_t noise(uint32_t index, uint32_t seed) {
+    uint32_t h = (index ^ seed) * 0x9E3779B1u;   // odd parts of the golden ratio and of sqrt 2
+    h = (h ^ (h >> 15)) * 0x6A09E667u;
+    h = (h ^ (h >> 13)) * 0x9E3779B1u;
+    return h ^ (h >> 16);
+}
+// |w| <= 448 (a rounding more at most) to an e4m3 number, up with the
+// probability of the part cut off; u is 16 uniform bits.
+__device__ __forceinline__ float round8(float w, uint32_t u) {
+    const float a = fabsf(w);
+    const float big = __uint_as_float((__float_as_uint(a) + (u << 4)) & ~0xfffffu);
+    const float small = floorf(__fadd_rn(__fmul_rn(a, 512.f), (float)u * 0x1p-16f)) * 0x1p-9f;
+    const float q = a >= 0x1p-6f ? big : small;
+    // (NaN stays NaN: it is neither below nor above)
+    const float c = q > 448.f ? 448.f : q;
+    return w < 0.f ? -c : c;
+}
+
+template <typename G> struct Four;
+template <> struct Four<float> { typedef f32x4 type; };
+template <> struct Four<bf16> { typedef bf16x4 type; };
+
+// Element e of lane `lane` in a block: four in a row (whole vectors), or one
+// of each 64 (any alignment, and the block that a tensor ends in).
+template <bool kVec> __device__ __forceinline__ int place(int lane, int e) { return kVec ? lane * 4 + e : lane + 64 * e; }
+
+template <typename X, bool kVec>
+__device__ __forceinline__ void load4(const X *p, int lane, int left, float (&o)[4]) {
+    if constexpr (kVec) {
+        const typename Four<X>::type w = *reinterpret_cast<const typename Four<X>::type *>(p + lane * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (float)w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = place<false>(lane, e) < left ? (float)p[place<false>(lane, e)] : 0.f;
+    }
+}
+template <typename X, bool kVec>
+__device__ __forceinline__ void store4(X *p, int lane, int left, const float (&v)[4]) {
+    if constexpr (kVec) {
+        typename Four<X>::type w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (X)v[e];
+        *reinterpret_cast<typename Four<X>::type *>(p + lane * 4) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (place<false>(lane, e) < left) p[place<false>(lane, e)] = (X)v[e];
+    }
+}
+// Four e4m3 codes
+template <bool kVec> __device__ __forceinline__ void load8(const uint8_t *p, int lane, int left, float (&o)[4]) {
+    if constexpr (kVec) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(p + lane * 4);
+        o[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+        o[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+        o[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+        o[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o[e] = place<false>(lane, e) < left ? __builtin_amdgcn_cvt_f32_fp8((int)p[place<false>(lane, e)], 0) : 0.f;
+    }
+}
+template <bool kVec> __device__ __forceinline__ void store8(uint8_t *p, int lane, int left, const float (&q)[4]) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+    if constexpr (kVec) {
+        *reinterpret_cast<uint32_t *>(p + lane * 4) = (uint32_t)w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (place<false>(lane, e) < left) p[place<false>(lane, e)] = (uint8_t)((uint32_t)w >> (8 * e));
+    }
+}
+
+struct Step {
+    float b1, c1, b2, c2, rate, root, eps, gs;
+    bool scaled;
+};
+
+// One element: m and v, the root of v, and the new p.
+__device__ __forceinline__ void update(const Step &k, float keep, float g, float &p, float &m, float &v, float &rv) {
+#pragma clang fp contract(off)
+    if (k.scaled) g = g * k.gs;
+    m = m * k.b1 + g * k.c1;
+    v = v * k.b2 + (g * g) * k.c2;
+    rv = __builtin_sqrtf(v);
+    p = p * keep - (m * k.rate) / (rv * k.root + k.eps);
+}
+
+template <typename G, bool kEight, bool kVec>
+__device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t base, int left, int lane) {
+    float g[4], p[4], m[4], v[4], rv[4];
+    load4<G, kVec>(static_cast<const G *>(t.g) + base, lane, left, g);
+    load4<float, kVec>(t.p + base, lane, left, p);
+    float *sc = t.scales + base / kBlockElems * 2;
+    if constexpr (kEight) {
+        load8<kVec>(static_cast<const uint8_t *>(t.m) + base, lane, left, m);
+        load8<kVec>(static_cast<const uint8_t *>(t.v) + base, lane, left, v);
+        const float sm = sc[0], sv = sc[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = __fmul_rn(m[e], sm);
+            const float r = __fmul_rn(v[e], sv);
+            v[e] = __fmul_rn(r, r);
+        }
+    } else {
+        load4<float, kVec>(static_cast<const float *>(t.m) + base, lane, left, m);
+        load4<float, kVec>(static_cast<const float *>(t.v) + base, lane, left, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) update(k, t.keep, g[e], p[e], m[e], v[e], rv[e]);
+    store4<float, kVec>(t.p + base, lane, left, p);
+    if (t.low) store4<bf16, kVec>(static_cast<bf16 *>(t.low) + base, lane, left, p);
+    if constexpr (!kEight) {
+        store4<float, kVec>(static_cast<float *>(t.m) + base, lane, left, m);
+        store4<float, kVec>(static_cast<float *>(t.v) + base, lane, left, v);
+    } else {
+        float am = 0.f, av = 0.f;
+        bool bad_m = false, bad_v = false;   // (fmaxf drops a NaN: it is carried beside the maximum)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (!kVec && place<false>(lane, e) >= left) { m[e] = 0.f; rv[e] = 0.f; }
+            am = fmaxf(am, fabsf(m[e]));
+            av = fmaxf(av, rv[e]);
+            bad_m = bad_m || m[e] != m[e];
+            bad_v = bad_v || rv[e] != rv[e];
+        }
+        am = wave_max(am);
+        av = wave_max(av);
+        if (__any(bad_m)) am = __builtin_nanf("");
+        if (__any(bad_v)) av = __builtin_nanf("");
+        const float nm = __fmul_rn(am, 1.f / 448.f), nv = __fmul_rn(av, 1.f / 448.f);
+        const float im = am > 0.f ? 1.f / nm : 0.f, iv = av > 0.f ? 1.f / nv : 0.f;
+        float qm[4], qv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t h = noise((uint32_t)(base + place<kVec>(lane, e)), t.seed);
+            qm[e] = round8(__fmul_rn(m[e], im), h & 0xffffu);
+            qv[e] = round8(__fmul_rn(rv[e], iv), h >> 16);
+            // a second moment that is not zero is not stored as zero: the next
+            // step would divide by almost nothing
+            if (rv[e] > 0.f && qv[e] < 0x1p-9f) qv[e] = 0x1p-9f;
+        }
+        store8<kVec>(static_cast<uint8_t *>(t.m) + base, lane, left, qm);
+        store8<kVec>(static_cast<uint8_t *>(t.v) + base, lane, left, qv);
+        if (lane == 0) { sc[0] = nm; sc[1] = nv; }
+    }
+}
+
+template <typename G, bool kEight>
+__global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int lo = 0, hi = a.count - 1;   // the tensor of this workgroup: the last that starts at or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.start[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+    }
+    const Tensor t = a.t[lo];
+    Step k{a.b1, a.c1, a.b2, a.c2, a.rate, a.root, a.eps, 1.f, a.grad_scale != nullptr};
+    if (k.scaled) k.gs = *a.grad_scale;
+    const int64_t base0 = (int64_t)((int)blockIdx.x - a.start[lo]) * kChunkElems + wave * kPer * kBlockElems;
+    // whole vectors where every array's are aligned
+    constexpr uintptr_t kState = kEight ? 3 : 15;
+    const bool vec = ((uintptr_t)t.p & 15) == 0 && ((uintptr_t)t.g & (4 * sizeof(G) - 1)) == 0 &&
+                     (((uintptr_t)t.m | (uintptr_t)t.v) & kState) == 0 && ((uintptr_t)t.low & 7) == 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int64_t base = base0 + j * kBlockElems;
+        if (base >= t.n) return;
+        const int left = (int)min((int64_t)kBlockElems, t.n - base);
+        if (vec && left == kBlockElems) block<G, kEight, true>(t, k, base, left, lane);
+        else block<G, kEight, false>(t, k, base, left, lane);
+    }
+}
+
+}  // namespace
+
+hipError_t launch(const Args &a, bool grad_f32, bool eight, hipStream_t s) {
+    const dim3 grid((unsigned)a.start[a.count]), blk(kWaves * 64);
+    if (grad_f32 && eight) k_adamw<float, true><<<grid, blk, 0, s>>>(a);
+    else if (grad_f32) k_adamw<float, false><<<grid, blk, 0, s>>>(a);
+    else if (eight) k_adamw<bf16, true><<<grid, blk, 0, s>>>(a);
+    else k_adamw<bf16, false><<<grid, blk, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace adamw
+}  // namespace m3

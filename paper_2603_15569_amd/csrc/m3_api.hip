@@ -16,6 +16,8 @@ namespace m3 {
 static thread_local int g_last_hip_error = 0;
 // bound of the single-pass kernels' look-back waits (m3_set_wait_limit)
 static std::atomic<uint32_t> g_spin_max{kSpinMaxDefault};
+void note_hip_error(hipError_t e) { g_last_hip_error = (int)e; }
+uint32_t wait_limit() { return g_spin_max.load(std::memory_order_relaxed); }
 
 static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static_assert(kCtlBytes == M3_CTL_BYTES, "control block size as documented");

@@ -125,6 +125,11 @@ template <class F> inline void for_segment_counts(int64_t most, int64_t slices, 
     }
 }
 
+// The front ends' shared state (m3_api.hip): notes a HIP error for
+// m3_last_hip_error, and the bound of look-back waits (m3_set_wait_limit).
+void note_hip_error(hipError_t e);
+uint32_t wait_limit();
+
 // default bound of a look-back wait (polls; ~seconds), then an error count
 constexpr uint32_t kSpinMaxDefault = 1u << 22;
 

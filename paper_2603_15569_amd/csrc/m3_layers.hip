@@ -1,0 +1,234 @@
+// C-ABI front end of the operators beside the scan: argument validation on the
+// host (before any HIP call), workspace layout, launches.
+#include <limits.h>
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "m3.h"
+#include "m3_adamw.h"
+#include "m3_glr.h"
+#include "m3_internal.h"
+
+using namespace m3;
+
+namespace {
+
+bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+m3_status launched(hipError_t e) {
+    if (e == hipSuccess) return M3_OK;
+    note_hip_error(e);
+    return M3_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+// Gated linear recurrence
+// ---------------------------------------------------------------------------
+
+static_assert(glr::kChunk == M3_GLR_CHUNK, "chunk as documented");
+
+// The token arrays' pointers: each on its element.  Channels a lane: two in
+// bf16 where every row and pair of channels stays on four bytes, else one.
+m3_status glr_vector(const m3_glr_dims *d, bool step, std::initializer_list<const void *> ptrs, bool z, int *V) {
+    const uintptr_t e = d->io == M3_F32 ? 4 : 2;
+    uintptr_t bits = 0;
+    for (const void *p : ptrs) bits |= (uintptr_t)p;
+    if (bits & (e - 1)) return M3_ERR_ALIGN;
+    int64_t odd = d->width | d->x_stride_b | d->r_stride_b | d->i_stride_b | (z ? d->z_stride_b : 0);
+    if (!step) odd |= d->x_stride_t | d->r_stride_t | d->i_stride_t | (z ? d->z_stride_t : 0);
+    *V = (e == 2 && odd % 2 == 0 && (bits & 3) == 0) ? 2 : 1;
+    return M3_OK;
+}
+
+m3_status check_glr(const m3_glr_dims *d, bool step) {
+    if (!d) return M3_ERR_NULL;
+    if (d->io != M3_F32 && d->io != M3_BF16) return M3_ERR_DTYPE;
+    if (d->flags != 0 || d->batch < 1 || d->width < 1 || (!step && d->seqlen < 0)) return M3_ERR_SHAPE;
+    const int64_t strides[] = {d->x_stride_b, d->x_stride_t, d->r_stride_b, d->r_stride_t,
+                               d->i_stride_b, d->i_stride_t, d->z_stride_b, d->z_stride_t};
+    // every element offset stays far inside 63 bits
+    constexpr int64_t kMost = INT64_C(1) << 56;
+    const int64_t L = step ? 1 : std::max<int64_t>(d->seqlen, 1);
+    if (d->batch > INT_MAX || d->width > INT_MAX || d->batch * d->width > kMost / L) return M3_ERR_SHAPE;
+    for (int64_t s : strides)
+        if (s < 0 || s > kMost / std::max(L, d->batch)) return M3_ERR_SHAPE;
+    if (step) return d->batch * d->width / 256 < INT_MAX ? M3_OK : M3_ERR_SHAPE;
+    // one workgroup a tile, counted in 31 bits (groups of 64 channels: the most)
+    const int64_t tiles = (d->seqlen + glr::kChunk - 1) / glr::kChunk, groups = (d->width + 63) / 64;
+    if (d->batch * groups > INT_MAX / std::max<int64_t>(tiles, 1)) return M3_ERR_SHAPE;
+    return M3_OK;
+}
+
+struct GlrLayout {
+    size_t inc, mapA, mapC, part, total;
+};
+GlrLayout glr_layout(const m3_glr_dims *d) {
+    const size_t tiles = (size_t)((d->seqlen + glr::kChunk - 1) / glr::kChunk);
+    const size_t words = round_up((size_t)d->batch * tiles * (size_t)d->width * sizeof(uint64_t), 256);
+    GlrLayout w;
+    w.inc = glr::kCtlBytes;
+    w.mapA = w.inc + words;
+    w.mapC = w.mapA + words;
+    w.part = w.mapC + words;
+    w.total = w.part + words;
+    return w;
+}
+
+// Arguments that the forward and the backward share
+template <class Args>
+void glr_common(const m3_glr_dims *d, const void *x, const void *r, const void *i, const float *A, const void *z,
+                int V, void *workspace, Args *a) {
+    a->x = x; a->r = r; a->i = i; a->z = z; a->A = A;
+    a->B = d->batch; a->L = d->seqlen; a->D = d->width;
+    a->G = (d->width + 64 * V - 1) / (64 * V);
+    a->tiles = (d->seqlen + glr::kChunk - 1) / glr::kChunk;
+    a->x_sb = d->x_stride_b; a->x_st = d->x_stride_t; a->r_sb = d->r_stride_b; a->r_st = d->r_stride_t;
+    a->i_sb = d->i_stride_b; a->i_st = d->i_stride_t; a->z_sb = d->z_stride_b; a->z_st = d->z_stride_t;
+    const GlrLayout w = glr_layout(d);
+    char *ws = static_cast<char *>(workspace);
+    a->ctl = reinterpret_cast<uint64_t *>(ws);
+    a->inc = reinterpret_cast<uint64_t *>(ws + w.inc);
+    a->mapA = reinterpret_cast<uint64_t *>(ws + w.mapA);
+    a->mapC = reinterpret_cast<uint64_t *>(ws + w.mapC);
+    a->spin_max = wait_limit();
+}
+
+}  // namespace
+
+extern "C" size_t m3_glr_workspace_bytes(const m3_glr_dims *d) {
+    return check_glr(d, false) == M3_OK ? glr_layout(d).total : 0;
+}
+
+extern "C" m3_status m3_glr_fwd(const m3_glr_dims *d, const void *x, const void *r, const void *i, const float *A,
+                                const void *z, const float *init_state, void *y, float *final_state, float *states,
+                                void *workspace, size_t workspace_bytes, void *stream) {
+    const m3_status s = check_glr(d, false);
+    if (s != M3_OK) return s;
+    if (!A || !final_state || (d->seqlen > 0 && (!x || !r || !i || !y))) return M3_ERR_NULL;
+    int V = 1;
+    const m3_status v = glr_vector(d, false, {x, r, i, z, y}, z != nullptr, &V);
+    if (v != M3_OK) return v;
+    for (const void *p : {(const void *)A, (const void *)init_state, (const void *)final_state, (const void *)states})
+        if (!aligned(p, 4)) return M3_ERR_ALIGN;
+    if (!aligned(workspace, 16)) return M3_ERR_ALIGN;
+    if (!workspace || workspace_bytes < glr_layout(d).total) return M3_ERR_WORKSPACE;
+    glr::FwdArgs a = {};
+    glr_common(d, x, r, i, A, z, V, workspace, &a);
+    a.init = init_state;
+    a.y = y;
+    a.final_state = final_state;
+    a.states = states;
+    return launched(glr::launch_fwd(a, d->io == M3_F32, V, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" m3_status m3_glr_bwd(const m3_glr_dims *d, const void *x, const void *r, const void *i, const float *A,
+                                const void *z, const float *states, const void *dy, const float *dfinal, void *dx,
+                                void *dr, void *di, void *dz, float *dA, float *dinit_state, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+    const m3_status s = check_glr(d, false);
+    if (s != M3_OK) return s;
+    if (!A || !dA || (d->seqlen > 0 && (!x || !r || !i || !states || !dy || !dx || !dr || !di || (z && !dz))))
+        return M3_ERR_NULL;
+    int V = 1;
+    const m3_status v = glr_vector(d, false, {x, r, i, z, dy, dx, dr, di, dz}, z != nullptr, &V);
+    if (v != M3_OK) return v;
+    for (const void *p : {(const void *)A, (const void *)states, (const void *)dfinal, (const void *)dA,
+                          (const void *)dinit_state})
+        if (!aligned(p, 4)) return M3_ERR_ALIGN;
+    if (!aligned(workspace, 16)) return M3_ERR_ALIGN;
+    const GlrLayout w = glr_layout(d);
+    if (!workspace || workspace_bytes < w.total) return M3_ERR_WORKSPACE;
+    glr::BwdArgs a = {};
+    glr_common(d, x, r, i, A, z, V, workspace, &a);
+    a.dy = dy; a.states = states; a.dfinal = dfinal;
+    a.dx = dx; a.dr = dr; a.di = di; a.dz = dz; a.dA = dA; a.dinit = dinit_state;
+    a.part = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + w.part);
+    return launched(glr::launch_bwd(a, d->io == M3_F32, V, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" m3_status m3_glr_step(const m3_glr_dims *d, float *state, const void *x, const void *r, const void *i,
+                                 const float *A, const void *z, void *y, void *stream) {
+    const m3_status s = check_glr(d, true);
+    if (s != M3_OK) return s;
+    if (!state || !x || !r || !i || !A || !y) return M3_ERR_NULL;
+    int V = 1;
+    const m3_status v = glr_vector(d, true, {x, r, i, z, y}, z != nullptr, &V);
+    if (v != M3_OK) return v;
+    if (!aligned(A, 4) || !aligned(state, 4)) return M3_ERR_ALIGN;
+    glr::StepArgs a = {};
+    a.state = state; a.x = x; a.r = r; a.i = i; a.z = z; a.A = A; a.y = y;
+    a.B = d->batch; a.D = d->width;
+    a.x_sb = d->x_stride_b; a.r_sb = d->r_stride_b; a.i_sb = d->i_stride_b; a.z_sb = d->z_stride_b;
+    return launched(glr::launch_step(a, d->io == M3_F32, V, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" m3_status m3_glr_check(const m3_glr_dims *d, const void *workspace, size_t workspace_bytes,
+                                  uint32_t *timeouts, void *stream) {
+    const m3_status s = check_glr(d, false);
+    if (s != M3_OK) return s;
+    if (!timeouts) return M3_ERR_NULL;
+    if (!workspace || workspace_bytes < glr_layout(d).total) return M3_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return M3_ERR_ALIGN;
+    if (d->seqlen <= glr::kChunk) {   // one tile a sequence: nothing waits
+        *timeouts = 0;
+        return M3_OK;
+    }
+    // ticket counter (the call count in its upper half), two timeout words
+    uint32_t ctl[4];
+    hipError_t e = hipMemcpyAsync(ctl, workspace, sizeof ctl, hipMemcpyDeviceToHost, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return launched(e);
+    *timeouts = ctl[2 + ((ctl[1] - 1u) & 1u)];
+    return M3_OK;
+}
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+
+extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_tensor *tensors, int64_t count,
+                                   const float *grad_scale, void *stream) {
+    if (!c || (count > 0 && !tensors)) return M3_ERR_NULL;
+    if (c->grad_dtype != M3_F32 && c->grad_dtype != M3_BF16) return M3_ERR_DTYPE;
+    if (count < 0 || c->step < 1 || (c->flags & ~M3_ADAMW_8BIT)) return M3_ERR_SHAPE;
+    if (!std::isfinite(c->lr) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) ||
+        !(c->eps >= 0.0) || !std::isfinite(c->eps))
+        return M3_ERR_SHAPE;
+    const bool eight = (c->flags & M3_ADAMW_8BIT) != 0, gf32 = c->grad_dtype == M3_F32;
+    if (!aligned(grad_scale, 4)) return M3_ERR_ALIGN;
+    for (int64_t k = 0; k < count; ++k) {   // all of them before the first launch
+        const m3_adamw_tensor &t = tensors[k];
+        if (t.n < 0 || !std::isfinite(t.decay)) return M3_ERR_SHAPE;
+        if (t.n / adamw::kChunkElems >= INT_MAX / (2 * adamw::kTensors)) return M3_ERR_SHAPE;
+        if (t.n == 0) continue;
+        if (!t.p || !t.g || !t.m || !t.v || (eight && !t.scales)) return M3_ERR_NULL;
+        if (!aligned(t.p, 4) || !aligned(t.g, gf32 ? 4 : 2) || !aligned(t.low, 2) || (eight && !aligned(t.scales, 4)) ||
+            (!eight && (!aligned(t.m, 4) || !aligned(t.v, 4))))
+            return M3_ERR_ALIGN;
+    }
+    adamw::Args a;
+    const double bc1 = 1.0 - std::pow(c->beta1, (double)c->step), bc2 = 1.0 - std::pow(c->beta2, (double)c->step);
+    a.b1 = (float)c->beta1; a.c1 = (float)(1.0 - c->beta1);
+    a.b2 = (float)c->beta2; a.c2 = (float)(1.0 - c->beta2);
+    a.rate = (float)(c->lr / bc1); a.root = (float)std::pow(bc2, -0.5); a.eps = (float)c->eps;
+    a.grad_scale = grad_scale;
+    for (int64_t k = 0; k < count;) {
+        a.count = 0;
+        a.start[0] = 0;
+        for (; k < count && a.count < adamw::kTensors; ++k) {
+            const m3_adamw_tensor &t = tensors[k];
+            if (t.n == 0) continue;
+            a.t[a.count] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, t.n, (float)(1.0 - c->lr * t.decay),
+                                         (uint32_t)(c->seed + (uint64_t)k)};
+            const int64_t chunks = (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
+            a.start[a.count + 1] = a.start[a.count] + (int32_t)chunks;
+            ++a.count;
+        }
+        if (a.count == 0) continue;
+        const m3_status s = launched(adamw::launch(a, gf32, eight, static_cast<hipStream_t>(stream)));
+        if (s != M3_OK) return s;
+    }
+    return M3_OK;
+}

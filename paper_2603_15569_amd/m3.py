@@ -48,6 +48,30 @@ class M3Prologue(ctypes.Structure):
 M3_OUT_NORM_NONE, M3_OUT_NORM_PRE_GATE, M3_OUT_NORM_POST_GATE = 0, 1, 2
 
 
+class M3GlrDims(ctypes.Structure):
+    """m3_glr_dims: sizes, io dtype and element strides of the gated linear recurrence."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("batch", "seqlen", "width")]
+                + [("io", ctypes.c_int32), ("flags", ctypes.c_int32)]
+                + [(f"{t}_stride_{a}", ctypes.c_int64) for t in "xriz" for a in "bt"])
+
+
+GLR_CHUNK = 128             # M3_GLR_CHUNK: tokens between two saved states
+M3_ADAMW_8BIT = 1
+
+
+class M3AdamwTensor(ctypes.Structure):
+    """m3_adamw_tensor: one tensor of the optimizer's table."""
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("low", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("decay", ctypes.c_double)]
+
+
+class M3AdamwConfig(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("grad_dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
 class M3Error(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"libm3 status {status}: {msg}")
@@ -58,6 +82,8 @@ EXPORTS = ("m3_scan_workspace_bytes", "m3_scan_fwd", "m3_scan_fwd_gated", "m3_sc
            "m3_scan_varlen_workspace_bytes", "m3_scan_varlen_check",
            "m3_step", "m3_step_gated", "m3_scan_check", "m3_set_wait_limit", "m3_scan_fwd_noalloc",
            "m3_scan_fwd_pro", "m3_step_pro", "m3_scan_bwd", "m3_scan_bwd_workspace_bytes",
+           "m3_glr_workspace_bytes", "m3_glr_fwd", "m3_glr_bwd", "m3_glr_step", "m3_glr_check",
+           "m3_adamw_step",
            "m3_status_string", "m3_last_hip_error")
 SCRATCH_BYTES = 256 << 20   # M3_SCRATCH_BYTES: the allocation-free scan's fixed workspace
 CTL_BYTES = 1280            # M3_CTL_BYTES: a scan workspace's control block (zero before first use)
@@ -105,6 +131,17 @@ def lib() -> ctypes.CDLL:
         L.m3_scan_fwd_noalloc.restype = ctypes.c_int
         L.m3_scan_check.argtypes = [dims_p, vp, ctypes.c_size_t, ctypes.POINTER(ctypes.c_uint32), vp]
         L.m3_scan_check.restype = ctypes.c_int
+        glr_p = ctypes.POINTER(M3GlrDims)
+        L.m3_glr_workspace_bytes.argtypes = [glr_p]
+        L.m3_glr_workspace_bytes.restype = ctypes.c_size_t
+        L.m3_glr_fwd.argtypes = [glr_p] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
+        L.m3_glr_bwd.argtypes = [glr_p] + [vp] * 14 + [vp, ctypes.c_size_t, vp]
+        L.m3_glr_step.argtypes = [glr_p] + [vp] * 7 + [vp]
+        L.m3_glr_check.argtypes = [glr_p, vp, ctypes.c_size_t, ctypes.POINTER(ctypes.c_uint32), vp]
+        L.m3_adamw_step.argtypes = [ctypes.POINTER(M3AdamwConfig), ctypes.POINTER(M3AdamwTensor),
+                                    ctypes.c_int64, vp, vp]
+        for name in ("glr_fwd", "glr_bwd", "glr_step", "glr_check", "adamw_step"):
+            getattr(L, "m3_" + name).restype = ctypes.c_int
         L.m3_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.m3_set_wait_limit.restype = None
         L.m3_status_string.argtypes = [ctypes.c_int]
@@ -505,3 +542,185 @@ def scan_bwd(x, Bm, Cm, dt, A, lam, theta, D, dy, chunk: int, dfinal=None, init_
                              _p(out["dA"]), _p(out["dlam"]), _p(out["dtheta"]), _p(out["dD"]),
                              _p(dinit), _p(workspace), workspace.numel(), _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------------------
+# Gated linear recurrence
+# ---------------------------------------------------------------------------
+
+def _rows(t: Optional[torch.Tensor], like: torch.Tensor, name: str):
+    """A pointer and the batch and token strides of a tensor shaped and typed like
+    `like` whose channels lie next to each other."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must have the shape, dtype and device of x")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
+    # (a stride over one element is never walked, whatever torch reports)
+    st = [t.stride(k) if t.shape[k] > 1 else 0 for k in range(t.dim() - 1)]
+    return t.data_ptr(), st[0], (st[1] if len(st) > 1 else 0)
+
+
+def _f32(t: Optional[torch.Tensor], shape, dev, name: str):
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != torch.float32 or t.device != dev:
+        raise ValueError(f"{name} must be fp32 {tuple(shape)} on {dev}")
+    return _p(t)
+
+
+def glr_dims(x, r=None, i=None, z=None) -> M3GlrDims:
+    """The dims of a recurrence over x [B, L, D] (a step: [B, D]) with gates r and i
+    and the output gate z."""
+    if x.dtype not in _IO:
+        raise ValueError("x must be fp32 or bf16")
+    step = x.dim() == 2
+    if x.dim() not in (2, 3):
+        raise ValueError(f"x must be [B, L, D] or [B, D], got {tuple(x.shape)}")
+    s = [v for name, t in (("x", x), ("r", r), ("i", i), ("z", z)) for v in _rows(t, x, name)[1:]]
+    return M3GlrDims(x.shape[0], 1 if step else x.shape[1], x.shape[-1], _IO[x.dtype], 0, *s)
+
+
+def glr_workspace(x, r=None, i=None, z=None) -> torch.Tensor:
+    """A workspace (zero-filled) for glr_fwd and glr_bwd of these inputs: keep it for
+    further calls, one at a time."""
+    n = int(lib().m3_glr_workspace_bytes(ctypes.byref(glr_dims(x, r, i, z))))
+    return torch.zeros(max(n, 16), dtype=torch.uint8, device=x.device)
+
+
+def glr_check(x, r, i, workspace, z=None, stream=None) -> int:
+    """m3_glr_check: look-back waits that gave up in the last call on `workspace`
+    (synchronises the stream)."""
+    n = ctypes.c_uint32(0)
+    _check(lib().m3_glr_check(ctypes.byref(glr_dims(x, r, i, z)), _p(workspace), workspace.numel(),
+                              ctypes.byref(n), _stream(stream)))
+    return int(n.value)
+
+
+def glr_fwd(x, r, i, A, z=None, init_state=None, save_states: bool = False, out=None,
+            workspace=None, stream=None):
+    """m3_glr_fwd: h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t with
+    log a_t = A sigmoid(r_t), y = h, or h o SiLU(z).  x, r, i, z [B, L, D] (bf16 or
+    fp32, channels next to each other, any batch and token strides), A [D] fp32.
+    Returns y [B, L, D], final_state [B, D] fp32 and, with `save_states`, the states
+    that glr_bwd takes.  `out` may supply (y, final_state)."""
+    d = glr_dims(x, r, i, z)
+    B, L, D = x.shape
+    f32 = dict(dtype=torch.float32, device=x.device)
+    y, fs = out if out is not None else (torch.empty((B, L, D), dtype=x.dtype, device=x.device),
+                                         torch.empty((B, D), **f32))
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("y must have the shape and dtype of x")
+    states = torch.empty((B, -(-L // GLR_CHUNK), D), **f32) if save_states else None
+    if workspace is None:
+        workspace = glr_workspace(x, r, i, z)
+    _check(lib().m3_glr_fwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
+                            _f32(A, (D,), x.device, "A"), None if z is None else z.data_ptr(),
+                            _f32(init_state, (B, D), x.device, "init_state"), _p(y),
+                            _f32(fs, (B, D), x.device, "final_state"), _p(states), _p(workspace),
+                            workspace.numel(), _stream(stream)))
+    return (y, fs, states) if save_states else (y, fs)
+
+
+def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = False,
+            workspace=None, stream=None):
+    """m3_glr_bwd: gradients of J = <dy, y> + <dfinal, final_state>, from the forward's
+    inputs and the states it saved.  Returns a dict: dx, dr, di (dz) in the io dtype,
+    dA [D] fp32 and, with `want_dinit`, dinit [B, D] fp32."""
+    d = glr_dims(x, r, i, z)
+    B, L, D = x.shape
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have the shape and dtype of x")
+    out = {k: torch.empty((B, L, D), dtype=x.dtype, device=x.device)
+           for k in ("dx", "dr", "di") + (("dz",) if z is not None else ())}
+    out["dA"] = torch.empty((D,), dtype=torch.float32, device=x.device)
+    if want_dinit:
+        out["dinit"] = torch.empty((B, D), dtype=torch.float32, device=x.device)
+    if workspace is None:
+        workspace = glr_workspace(x, r, i, z)
+    _check(lib().m3_glr_bwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
+                            _f32(A, (D,), x.device, "A"), None if z is None else z.data_ptr(),
+                            _f32(states, (B, -(-L // GLR_CHUNK), D), x.device, "states"), _p(dy),
+                            _f32(dfinal, (B, D), x.device, "dfinal"), _p(out["dx"]), _p(out["dr"]),
+                            _p(out["di"]), _p(out.get("dz")), _p(out["dA"]), _p(out.get("dinit")),
+                            _p(workspace), workspace.numel(), _stream(stream)))
+    return out
+
+
+def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
+    """m3_glr_step: one token, x, r, i, z [B, D]; advances `state` [B, D] fp32 in
+    place and returns y [B, D]."""
+    d = glr_dims(x, r, i, z)
+    if x.dim() != 2:
+        raise ValueError(f"x must be [B, D], got {tuple(x.shape)}")
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("y must have the shape and dtype of x")
+    _check(lib().m3_glr_step(ctypes.byref(d), _f32(state, x.shape, x.device, "state"), x.data_ptr(),
+                             r.data_ptr(), i.data_ptr(), _f32(A, x.shape[1:], x.device, "A"),
+                             None if z is None else z.data_ptr(), _p(y), _stream(stream)))
+    return y
+
+
+# ---------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------
+
+class AdamWTable:
+    """The tensors of an optimizer step as m3_adamw_step takes them (built by
+    adamw_table; holds them, so that their memory stays)."""
+
+    def __init__(self, array, grad_dtype, flags, tensors):
+        self.array, self.grad_dtype, self.flags, self.tensors = array, grad_dtype, flags, tensors
+
+
+def adamw_table(params, grads, exp_avg, exp_avg_sq, weight_decay=0.0, low=None, scales=None):
+    """A table of tensors for adamw_step: lists of fp32 params, of grads (fp32 or bf16)
+    and of the states, shaped like the params; `weight_decay` a number or one per
+    tensor; `low` bf16 copies of the params to write.  The states are fp32, or with
+    `scales` (fp32 [ceil(n / 256), 2] each) torch.float8_e4m3fn: e4m3 codes of m and of
+    sqrt(v).  Zeros are the first step's states."""
+    n = len(params)
+    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+    lists = [grads, exp_avg, exp_avg_sq, decay] + [v for v in (low, scales) if v is not None]
+    if any(len(v) != n for v in lists):
+        raise ValueError("adamw_table takes lists of one length")
+    eight = scales is not None
+    state = torch.float8_e4m3fn if eight else torch.float32
+    gtype = grads[0].dtype if n else torch.float32
+    if gtype not in _IO:
+        raise ValueError("gradients are fp32 or bf16")
+    array = (M3AdamwTensor * n)()
+    for k in range(n):
+        p = params[k]
+        want = [("param", p, torch.float32), ("gradient", grads[k], gtype), ("exp_avg", exp_avg[k], state),
+                ("exp_avg_sq", exp_avg_sq[k], state)]
+        if low is not None:
+            want.append(("low", low[k], torch.bfloat16))
+        for name, t, dtype in want:
+            if t.dtype != dtype or t.shape != p.shape or t.device != p.device:
+                raise ValueError(f"tensor {k}: {name} must be {dtype} {tuple(p.shape)} on {p.device}")
+        if eight and (scales[k].dtype != torch.float32
+                      or tuple(scales[k].shape) != (-(-p.numel() // 256), 2)):
+            raise ValueError(f"tensor {k}: scales must be fp32 [ceil(n / 256), 2]")
+        array[k] = M3AdamwTensor(_p(p), _p(grads[k]), _p(exp_avg[k]), _p(exp_avg_sq[k]),
+                                 _p(low[k]) if low is not None else None,
+                                 _p(scales[k]) if eight else None, p.numel(), float(decay[k]))
+    held = (list(params), list(grads), list(exp_avg), list(exp_avg_sq), low and list(low),
+            scales and list(scales))
+    return AdamWTable(array, _IO[gtype], M3_ADAMW_8BIT if eight else 0, held)
+
+
+def adamw_step(table: AdamWTable, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+               grad_scale=None, seed: int = 0, stream=None) -> None:
+    """m3_adamw_step: one AdamW step (the `step`-th, from 1) over the table's tensors, in
+    place.  `grad_scale` is a device scalar that every gradient is multiplied by (None:
+    1); `seed` feeds the 8-bit states' stochastic rounding: another for every step."""
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("grad_scale is one fp32 number on the device")
+    c = M3AdamwConfig(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step),
+                      int(seed) & (2 ** 64 - 1), table.grad_dtype, table.flags)
+    _check(lib().m3_adamw_step(ctypes.byref(c), table.array, len(table.array),
+                               None if grad_scale is None else grad_scale.data_ptr(), _stream(stream)))
