@@ -549,6 +549,47 @@ m3_status m3_glr_check(const m3_glr_dims *dims, const void *workspace, size_t wo
                        uint32_t *timeouts, void *stream);
 
 /*
+ * Gated feed-forward block (the block between two mixers of the stack):
+ *
+ *     g = x Wg^T,  u = x Wu^T,  h = act(g) o u,  y = h Wd^T
+ *
+ * act is SiLU (M3_ACT_SILU) or GELU in its tanh form (M3_ACT_GELU).  x and dy
+ * [tokens][dmodel] with row strides (elements) of at least dmodel, Wg and Wu
+ * [dff][dmodel], Wd [dmodel][dff], y and dx [tokens][dmodel]: io dtype, all
+ * but x and dy contiguous.  Products are accumulated in fp32; h (and in the
+ * backward dg and du) is rounded once to the io dtype between the products,
+ * g and u are not.
+ *
+ * m3_ffn_bwd: gradients of J given dy = dJ/dy, from the forward's inputs only
+ * (g and u are formed again, so a forward keeps nothing for it):
+ *     dh = dy Wd,  du = dh o act(g),  dg = dh o u o act'(g)
+ *     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h
+ * in the io dtype.  Everything is overwritten.
+ *
+ * tokens 0 is allowed (the weight gradients are then zero; x, y, dy and dx may
+ * be NULL).  Workspace: m3_ffn_workspace_bytes(dims, backward) bytes, no
+ * initialisation (0 on invalid dims).  Rows that do not start on 16 bytes (odd
+ * sizes or strides) are first copied there to rows that do.  Deterministic.
+ * Alignment: the workspace 16 bytes; weights 16 bytes where their rows are
+ * whole 16-byte pieces; else the element's (else M3_ERR_ALIGN).  dmodel, dff
+ * and the strides are at most 2^20.  Outputs must not overlap inputs.
+ */
+#define M3_ACT_SILU 0
+#define M3_ACT_GELU 1
+typedef struct {
+    int64_t tokens, dmodel, dff;    /* tokens >= 0, the others >= 1           */
+    int32_t io;                     /* m3_dtype                               */
+    int32_t act;                    /* M3_ACT_*                               */
+    int64_t x_stride, dy_stride;    /* elements between rows (dy_stride: backward) */
+} m3_ffn_dims;
+size_t m3_ffn_workspace_bytes(const m3_ffn_dims *dims, int backward);
+m3_status m3_ffn_fwd(const m3_ffn_dims *dims, const void *x, const void *Wg, const void *Wu,
+                     const void *Wd, void *y, void *workspace, size_t workspace_bytes, void *stream);
+m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, const void *Wu,
+                     const void *Wd, const void *dy, void *dx, void *dWg, void *dWu, void *dWd,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * AdamW over many tensors (decoupled weight decay), in place, one launch for
  * every 48 tensors, nothing else on the device:
  *

@@ -1,0 +1,42 @@
+// Kernel arguments of the gated feed-forward block (m3_ffn.hip), already
+// validated and laid out by the front end (m3_layers.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace m3 {
+namespace ffn {
+
+// C[m][n] = sum over k of A(m, k) B(n, k).  An operand lies either with k
+// next to each other ([m][k]) or with its own axis so ([k][m], "turned").
+// Rows start on 16 bytes.
+struct GemmArgs {
+    const void *a[2], *b[2];   // two: two products summed (nseg), two products (grid z), or the two gates (b)
+    int64_t lda, ldb;          // elements
+    int64_t M, N, K;
+    int nseg;
+    void *c[2];
+    int64_t ldc;
+    // gates: h, dg, du with rows of ldc elements (columns N .. ldc - 1 are written as zeros), dh in fp32
+    void *dg, *du;
+    const float *dh;
+    int gelu;
+    int tiles_m, tiles_n;
+};
+
+enum Kind {
+    kStore,      // C in the io dtype
+    kStoreF32,   // C in fp32
+    kGate,       // h = act(g) u
+    kGateBwd,    // h, dg, du from g, u and dh
+};
+
+// C = A B (both as [row][k], or B or both turned), the two gates
+hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s);
+// rows of `cols` elements copied to rows of `ld`, zeros after
+hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
+                      hipStream_t s);
+
+}  // namespace ffn
+}  // namespace m3

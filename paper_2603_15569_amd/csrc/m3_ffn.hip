@@ -1,0 +1,383 @@
+// Gated feed-forward block on gfx950: y = (act(x Wg^T) o (x Wu^T)) Wd^T and its
+// gradients, as matrix products with the activation in their epilogues.
+//
+// One tiled product serves every part: a workgroup forms a BM x BN tile of C,
+// its operands streamed through LDS 128 bytes of k at a time by loads that go
+// straight there, two stages deep, and multiplied on the matrix cores (bf16:
+// 16x16x32, fp32: 16x16x4, accumulated in fp32).  The two gates are one
+// product whose B tile holds rows of Wg and of Wu in turn, so that a lane
+// holds g and u of the same elements.  Operands whose k runs down the rows
+// (the gradients') are read out of LDS with the transposing read.
+//
+// Edges: buffer loads return zero past the end of an operand, so rows past M,
+// N or (turned) K need no masks; k past K within a row is sent out of range.
+#include "m3_device.h"
+#include "m3_ffn.h"
+#include "m3_scan_common.h"
+
+namespace m3 {
+namespace ffn {
+namespace {
+
+using scan::Rsrc;
+using scan::make_rsrc;
+
+constexpr int kRowBytes = 128;              // bytes of k a stage
+constexpr uint32_t kOut = 0x80000000u;      // an offset past every operand's end
+
+// Where a 16-byte piece of an LDS row is stored: pieces are moved within their
+// row so that the rows one read takes lie on different banks.
+// [row][k] tiles: rows of eight pieces, piece g of row r at g ^ spread(r).
+template <bool kPair> __device__ __forceinline__ int spread(int row) {
+    return kPair ? (row & 3) | (row >> 1 & 4) : row & 7;
+}
+// [k][row] tiles: blocks of 16 elements, block b of k-row r at b ^ turn(r).
+template <typename T> __device__ __forceinline__ int turn(int k) {
+    return sizeof(T) == 2 ? (k & 3) | (k >> 1 & 4) : k >> 2 & 3;
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// One 16-byte piece a lane from `off` bytes into a buffer to LDS: lane l's goes
+// to `to` + 16 l.
+__device__ __forceinline__ void load_lds(Rsrc r, uint32_t off, char *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)to, 16, (int)off, 0, 0, 0);
+}
+
+// An operand tile's loads: ROWS rows of the operand by 128 bytes of k.
+template <typename T, int ROWS, int NW, bool kTurned, bool kPair> struct Tile {
+    static constexpr int EL = 16 / sizeof(T), BK = kRowBytes / sizeof(T);
+    static constexpr int PR = ROWS * sizeof(T) / 16;               // pieces of a turned row
+    static constexpr int RPI = kTurned ? 64 / (PR < 64 ? PR : 64) : 8;   // LDS rows an instruction
+    static constexpr int NI = ROWS * kRowBytes / 1024 / NW;        // instructions a wave
+    static_assert(ROWS * kRowBytes % (1024 * NW) == 0 && PR <= 64, "whole instructions");
+    uint32_t off[NI];
+    // k (turned: the row's place in the tile) of the lane's piece, and its offset
+    __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int row0 = (j * NW + wave) * RPI;
+            if constexpr (kTurned) {
+                const int row = row0 + lane / PR, pos = lane % PR;
+                constexpr int PB = 16 * sizeof(T) / 16;            // pieces a block of 16 elements
+                const int src = (pos / PB ^ turn<T>(row)) * PB + pos % PB;
+                off[j] = (uint32_t)(row * (int)(ld * sizeof(T)) + src * 16);
+            } else {
+                const int row = row0 + lane / 8, src = (lane % 8) ^ spread<kPair>(row);
+                off[j] = (uint32_t)(row * (int)(ld * sizeof(T)) + src * 16);
+            }
+        }
+    }
+    // k of instruction j's piece in a [row][k] tile
+    __device__ __forceinline__ int k_of(int j, int wave, int lane) const {
+        const int row = (j * NW + wave) * 8 + lane / 8;
+        return ((lane % 8) ^ spread<kPair>(row)) * EL;
+    }
+};
+
+// Bytes that up to `most` of `rows` rows take whose last ends with the 16-byte
+// piece that holds its element cols - 1 (rows are padded to whole pieces).
+template <typename T> __device__ __forceinline__ uint32_t span(int64_t rows, int64_t ld, int64_t cols, int most) {
+    constexpr int64_t EL = 16 / sizeof(T);
+    const int64_t r = min(rows, (int64_t)most);
+    return r <= 0 ? 0u : (uint32_t)(((r - 1) * ld + (cols + EL - 1) / EL * EL) * (int64_t)sizeof(T));
+}
+
+// Operand fragments of 16 rows by 64 bytes of k (kk = 0, 1): lane (q, l16) holds
+// 16 bytes of k of row l16.
+template <typename T, bool kPair>
+__device__ __forceinline__ f32x4 frag(const char *tile, int row, int kk, int q) {
+    return *reinterpret_cast<const f32x4 *>(tile + row * kRowBytes + ((kk * 4 + q) ^ spread<kPair>(row)) * 16);
+}
+template <typename T, int ROWS>
+__device__ __forceinline__ f32x4 frag_turned(const char *tile, int c0, int kk, int q, int l16) {
+    constexpr int W = ROWS * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+        const int k = kk * 32 + 8 * q + l16 / 4;
+        const char *p0 = tile + k * W + ((c0 / 16) ^ turn<T>(k)) * 32 + (l16 % 4) * 8;
+        const char *p1 = tile + (k + 4) * W + ((c0 / 16) ^ turn<T>(k + 4)) * 32 + (l16 % 4) * 8;
+        const bf16x4 lo = scan::lds_tr4(reinterpret_cast<const bf16 *>(p0));
+        const bf16x4 hi = scan::lds_tr4(reinterpret_cast<const bf16 *>(p1));
+        return __builtin_bit_cast(f32x4, scan::cat4(lo, hi));
+    } else {
+        f32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = kk * 16 + 4 * q + j;
+            v[j] = *reinterpret_cast<const float *>(tile + k * W + ((c0 / 16) ^ turn<T>(k)) * 64 + l16 * 4);
+        }
+        return v;
+    }
+}
+template <typename T> __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+    if constexpr (sizeof(T) == 2) {
+        return Mma<bf16>::mma(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = Mma<float>::mma(a[j], b[j], c);
+        return c;
+    }
+}
+
+// act(g) = g sigmoid(p) and its derivative sigmoid(p) + g sigmoid(p) (1 - sigmoid(p)) p':
+// SiLU with p = g, GELU's tanh form with p = 2 sqrt(2 / pi) (g + 0.044715 g^3)
+__device__ __forceinline__ float act(float g, bool gelu, float &slope) {
+    constexpr float kS = 1.59576912160573071176f, kC = 0.044715f;
+    const float p = gelu ? kS * g * fmaf(kC, g * g, 1.f) : g;
+    const float dp = gelu ? kS * fmaf(3.f * kC, g * g, 1.f) : 1.f;
+    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-p));
+    const float f = g * s;
+    // (where s (1 - s) has gone to zero, g p' may have overflowed: their product is zero)
+    const float t = 1.f - s;
+    slope = fmaf(t > 0.f && s > 0.f ? f * dp : 0.f, t, s);
+    return s > 0.f ? f : 0.f * s;
+}
+
+template <typename T, int BM, int BN, int NWM, int NWN, bool kAT, bool kBT, Kind KIND>
+__global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
+    constexpr int NW = NWM * NWN, BK = kRowBytes / sizeof(T);
+    constexpr int WM = BM / NWM, WN = BN / NWN, MT = WM / 16, NT = WN / 16;
+    constexpr bool kGates = KIND == kGate || KIND == kGateBwd;
+    constexpr bool kPair = !kBT;                 // n in the order that gives a lane eight in a row
+    constexpr int NB = kGates ? BN / 2 : BN;     // columns of C a tile
+    static_assert(!kGates || (WN == 64 && !kAT && !kBT), "a wave's 32 columns of g, then of u");
+    __shared__ __attribute__((aligned(1024))) char lds[2][(BM + BN) * kRowBytes];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wm = wave / NWN, wn = wave % NWN, l16 = lane & 15, q = lane / 16;
+
+    // Workgroups go to the XCDs in turn: each XCD gets a run of tiles, eight
+    // rows of tiles at a time, column by column, so that what runs together
+    // on an XCD shares operand rows in its L2.
+    const int total = g.tiles_m * g.tiles_n, id = (int)blockIdx.x;
+    const int xcd = id % 8, per = total / 8, rem = total % 8;
+    const int t = xcd * per + min(xcd, rem) + id / 8;
+    constexpr int GM = 8;
+    const int grp = t / (GM * g.tiles_n), in = t % (GM * g.tiles_n);
+    const int gm = min(GM, g.tiles_m - grp * GM);
+    const int64_t m0 = (int64_t)(grp * GM + in % gm) * BM, n0 = (int64_t)(in / gm) * NB;
+    const int z = (int)blockIdx.z;
+
+    Tile<T, BM, NW, kAT, false> ta;
+    Tile<T, BN, NW, kBT, kPair> tb;
+    ta.init(g.lda, wave, lane);
+    if constexpr (kGates) {
+        // LDS row r: column r % 32 of wave r / 64's part of Wg (r % 64 < 32) or Wu
+#pragma unroll
+        for (int j = 0; j < tb.NI; ++j) {
+            const int row = (j * NW + wave) * 8 + lane / 8;
+            tb.off[j] = (uint32_t)((row / 64 * 32 + row % 32) * (int)(g.ldb * sizeof(T)) + ((lane % 8) ^ spread<kPair>(row)) * 16);
+        }
+    } else {
+        tb.init(g.ldb, wave, lane);
+    }
+
+    const int nk = (int)((g.K + BK - 1) / BK), steps = nk * g.nseg;
+    auto load = [&](int it) {
+        const int seg = it >= nk ? 1 : 0;
+        const int64_t k0 = (int64_t)(it - seg * nk) * BK;
+        const bool tail = k0 + BK > g.K;
+        char *stage = lds[it & 1];
+        const T *pa = static_cast<const T *>(g.a[kGates ? 0 : z + seg]);
+        const Rsrc ra = kAT ? make_rsrc(pa + k0 * g.lda + m0, span<T>(g.K - k0, g.lda, g.M - m0, BK))
+                            : make_rsrc(pa + m0 * g.lda + k0, span<T>(g.M - m0, g.lda, g.K - k0, BM));
+#pragma unroll
+        for (int j = 0; j < ta.NI; ++j) {
+            uint32_t off = ta.off[j];
+            if constexpr (!kAT)
+                if (tail && k0 + ta.k_of(j, wave, lane) >= g.K) off = kOut;
+            load_lds(ra, off, stage + (j * NW + wave) * 1024);
+        }
+        stage += BM * kRowBytes;
+        if constexpr (kGates) {
+#pragma unroll
+            for (int j = 0; j < tb.NI; ++j) {
+                const int which = (j * NW + wave) * 8 % 64 / 32;
+                const T *pb = static_cast<const T *>(which ? g.b[1] : g.b[0]);
+                const Rsrc rb = make_rsrc(pb + n0 * g.ldb + k0, span<T>(g.N - n0, g.ldb, g.K - k0, NB));
+                uint32_t off = tb.off[j];
+                if (tail && k0 + tb.k_of(j, wave, lane) >= g.K) off = kOut;
+                load_lds(rb, off, stage + (j * NW + wave) * 1024);
+            }
+        } else {
+            const T *pb = static_cast<const T *>(g.b[z + seg]);
+            const Rsrc rb = kBT ? make_rsrc(pb + k0 * g.ldb + n0, span<T>(g.K - k0, g.ldb, g.N - n0, BK))
+                                : make_rsrc(pb + n0 * g.ldb + k0, span<T>(g.N - n0, g.ldb, g.K - k0, BN));
+#pragma unroll
+            for (int j = 0; j < tb.NI; ++j) {
+                uint32_t off = tb.off[j];
+                if constexpr (!kBT)
+                    if (tail && k0 + tb.k_of(j, wave, lane) >= g.K) off = kOut;
+                load_lds(rb, off, stage + (j * NW + wave) * 1024);
+            }
+        }
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (steps > 0) load(0);
+    for (int it = 0; it < steps; ++it) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's pieces of the stage have landed (vmcnt 0)
+        __syncthreads();                      // everyone's have, and the other stage has been read
+        if (it + 1 < steps) load(it + 1);
+        const char *sa = lds[it & 1], *sb = sa + BM * kRowBytes;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            f32x4 fb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if constexpr (kBT) {
+                    fb[j] = frag_turned<T, BN>(sb, wn * WN + 16 * j, kk, q, l16);
+                } else {
+                    // the tile's row r is column 8 (r / 4) + r % 4 (+ 4 in odd tiles) of 32
+                    fb[j] = frag<T, kPair>(sb, wn * WN + j / 2 * 32 + l16 / 4 * 8 + l16 % 4 + j % 2 * 4, kk, q);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const f32x4 fa = kAT ? frag_turned<T, BM>(sa, wm * WM + 16 * i, kk, q, l16)
+                                     : frag<T, false>(sa, wm * WM + 16 * i + l16, kk, q);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa, acc[i][j]);
+            }
+        }
+    }
+
+    // A lane holds row m = l16 of each 16-row tile, and four columns of each of
+    // the NT column tiles: 4 q .. 4 q + 3, or (pairs of tiles) 8 q .. 8 q + 7.
+    const int64_t mw = m0 + wm * WM;
+    if constexpr (kGates) {
+        const int64_t n = n0 + wn * 32 + 8 * q;      // (ldc is a multiple of eight, bf16, or four)
+        if (n >= g.ldc) return;
+        const bool gelu = g.gelu != 0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int64_t m = mw + 16 * i + l16;
+            if (m >= g.M) continue;
+            float h[8], dg[8], du[8], dh[8];
+            const int64_t at = m * g.ldc + n;
+            const int w = (int)min((int64_t)8, g.ldc - n);   // 8, or 4 in fp32
+            if constexpr (KIND == kGateBwd) {
+#pragma unroll
+                for (int p = 0; p < 8; p += 4) {
+                    const f32x4 v = p < w ? *reinterpret_cast<const f32x4 *>(g.dh + at + p) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dh[p + e] = v[e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float gv = acc[i][e / 4][e % 4], uv = acc[i][2 + e / 4][e % 4];
+                float slope;
+                const float f = act(gv, gelu, slope);
+                h[e] = f * uv;
+                if constexpr (KIND == kGateBwd) {
+                    du[e] = dh[e] * f;
+                    dg[e] = dh[e] * uv * slope;
+                }
+            }
+            auto put = [&](void *dst, const float (&v)[8]) {
+                T *p = static_cast<T *>(dst) + at;
+                if constexpr (sizeof(T) == 2) {
+                    bf16x8 o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = (bf16)v[e];
+                    *reinterpret_cast<bf16x8 *>(p) = o;
+                } else {
+                    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+                    if (w == 8) *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                }
+            };
+            put(g.c[0], h);
+            if constexpr (KIND == kGateBwd) {
+                put(g.dg, dg);
+                put(g.du, du);
+            }
+        }
+    } else {
+        typedef typename std::conditional<KIND == kStoreF32, float, T>::type O;
+        O *c = static_cast<O *>(g.c[z]);
+        constexpr int RUN = kPair ? 8 : 4;         // columns in a row a lane
+        const bool whole = g.ldc * sizeof(O) % 16 == 0 && ((uintptr_t)c & 15) == 0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int64_t m = mw + 16 * i + l16;
+            if (m >= g.M) continue;
+#pragma unroll
+            for (int p = 0; p < NT; p += RUN / 4) {
+                const int64_t n = n0 + wn * WN + (kPair ? p / 2 * 32 + 8 * q : 16 * p + 4 * q);
+                if (n >= g.N) continue;
+                float v[RUN];
+#pragma unroll
+                for (int e = 0; e < RUN; ++e) v[e] = acc[i][p + e / 4][e % 4];
+                O *o = c + m * g.ldc + n;
+                if (whole && n + RUN <= g.N) {
+                    if constexpr (sizeof(O) == 4) {
+#pragma unroll
+                        for (int e = 0; e < RUN; e += 4) *reinterpret_cast<f32x4 *>(o + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                    } else {
+                        typedef __bf16 piece __attribute__((ext_vector_type(RUN)));
+                        piece w;
+#pragma unroll
+                        for (int e = 0; e < RUN; ++e) w[e] = (bf16)v[e];
+                        *reinterpret_cast<piece *>(o) = w;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < RUN; ++e)
+                        if (n + e < g.N) o[e] = (O)v[e];
+                }
+            }
+        }
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void k_pad(const T *src, int64_t src_ld, T *dst, int64_t dst_ld,
+                                                                    int64_t cols) {
+    const int64_t row = blockIdx.x;
+    for (int64_t k = threadIdx.x; k < dst_ld; k += 256) dst[row * dst_ld + k] = k < cols ? src[row * src_ld + k] : (T)0.f;
+}
+
+template <typename T, int BM, int BN, int NWM, int NWN, bool kAT, bool kBT, Kind KIND>
+hipError_t run(GemmArgs g, int batch, hipStream_t s) {
+    constexpr int NB = KIND == kGate || KIND == kGateBwd ? BN / 2 : BN;
+    const int64_t n = KIND == kGate || KIND == kGateBwd ? g.ldc : g.N;
+    g.tiles_m = (int)((g.M + BM - 1) / BM);
+    g.tiles_n = (int)((n + NB - 1) / NB);
+    k_gemm<T, BM, BN, NWM, NWN, kAT, kBT, KIND>
+        <<<dim3((unsigned)(g.tiles_m * g.tiles_n), 1, (unsigned)batch), dim3(NWM * NWN * 64), 0, s>>>(g);
+    return hipGetLastError();
+}
+
+template <typename T, bool kAT, bool kBT, Kind KIND> hipError_t pick(const GemmArgs &g, int batch, hipStream_t s) {
+    if constexpr (sizeof(T) == 2) return run<T, 256, 256, 2, 4, kAT, kBT, KIND>(g, batch, s);
+    else return run<T, 128, 128, 2, 2, kAT, kBT, KIND>(g, batch, s);
+}
+
+template <typename T> hipError_t dispatch(const GemmArgs &g, bool at, bool bt, Kind kind, int batch, hipStream_t s) {
+    if (kind == kGate) return pick<T, false, false, kGate>(g, batch, s);
+    if (kind == kGateBwd) return pick<T, false, false, kGateBwd>(g, batch, s);
+    if (kind == kStoreF32) return pick<T, false, true, kStoreF32>(g, batch, s);
+    if (at) return pick<T, true, true, kStore>(g, batch, s);
+    return bt ? pick<T, false, true, kStore>(g, batch, s) : pick<T, false, false, kStore>(g, batch, s);
+}
+
+}  // namespace
+
+hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s) {
+    return f32 ? dispatch<float>(g, at, bt, kind, batch, s) : dispatch<bf16>(g, at, bt, kind, batch, s);
+}
+hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
+                      hipStream_t s) {
+    const dim3 grid((unsigned)rows), block(256);
+    if (f32) k_pad<float><<<grid, block, 0, s>>>(static_cast<const float *>(src), src_ld, static_cast<float *>(dst), dst_ld, cols);
+    else k_pad<bf16><<<grid, block, 0, s>>>(static_cast<const bf16 *>(src), src_ld, static_cast<bf16 *>(dst), dst_ld, cols);
+    return hipGetLastError();
+}
+
+}  // namespace ffn
+}  // namespace m3

@@ -8,6 +8,7 @@
 
 #include "m3.h"
 #include "m3_adamw.h"
+#include "m3_ffn.h"
 #include "m3_glr.h"
 #include "m3_internal.h"
 
@@ -182,6 +183,165 @@ extern "C" m3_status m3_glr_check(const m3_glr_dims *d, const void *workspace, s
     if (e != hipSuccess) return launched(e);
     *timeouts = ctl[2 + ((ctl[1] - 1u) & 1u)];
     return M3_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Gated feed-forward block
+// ---------------------------------------------------------------------------
+
+namespace {
+
+m3_status check_ffn(const m3_ffn_dims *d, bool bwd) {
+    if (!d) return M3_ERR_NULL;
+    if (d->io != M3_F32 && d->io != M3_BF16) return M3_ERR_DTYPE;
+    constexpr int64_t kMost = INT64_C(1) << 20;   // (a tile's rows within 31-bit offsets)
+    if (d->tokens < 0 || d->dmodel < 1 || d->dff < 1 || d->dmodel > kMost || d->dff > kMost) return M3_ERR_SHAPE;
+    if (d->tokens > (INT64_C(1) << 40) / std::max(d->dmodel, d->dff)) return M3_ERR_SHAPE;
+    if (d->act != M3_ACT_SILU && d->act != M3_ACT_GELU) return M3_ERR_SHAPE;
+    if (d->x_stride < d->dmodel || d->x_stride > kMost) return M3_ERR_SHAPE;
+    if (bwd && (d->dy_stride < d->dmodel || d->dy_stride > kMost)) return M3_ERR_SHAPE;
+    // one workgroup a tile of 64 (gates) or 128 columns and 128 rows, counted in 31 bits
+    const int64_t rows = std::max(d->tokens, std::max(d->dmodel, d->dff)) / 128 + 1;
+    if (rows > INT_MAX / (std::max(d->dmodel, d->dff) / 64 + 1)) return M3_ERR_SHAPE;
+    return M3_OK;
+}
+
+// Rows in the workspace start on 16 bytes: their lengths are whole pieces.
+struct FfnLayout {
+    int64_t Dp, Fp;
+    bool pad_d, pad_f;             // weights with rows of dmodel, of dff, are copied
+    size_t x, dy, wg, wu, wd, h, dg, du, dh, total;
+};
+FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
+    const int64_t e = d->io == M3_F32 ? 4 : 2, el = 16 / e;
+    FfnLayout w = {};
+    w.Dp = (d->dmodel + el - 1) / el * el;
+    w.Fp = (d->dff + el - 1) / el * el;
+    w.pad_d = w.Dp != d->dmodel;
+    w.pad_f = w.Fp != d->dff;
+    size_t at = 0;
+    auto take = [&](int64_t rows, int64_t cols, int64_t bytes) {
+        const size_t here = at;
+        at = round_up(at + (size_t)(rows * cols * bytes), 256);
+        return here;
+    };
+    w.x = take(d->tokens, w.Dp, e);                       // (used where x's rows need it)
+    w.dy = bwd ? take(d->tokens, w.Dp, e) : 0;
+    w.wg = take(w.pad_d ? d->dff : 0, w.Dp, e);
+    w.wu = take(w.pad_d ? d->dff : 0, w.Dp, e);
+    w.wd = take(w.pad_f ? d->dmodel : 0, w.Fp, e);
+    w.h = take(d->tokens, w.Fp, e);
+    w.dg = bwd ? take(d->tokens, w.Fp, e) : 0;
+    w.du = bwd ? take(d->tokens, w.Fp, e) : 0;
+    w.dh = bwd ? take(d->tokens, w.Fp, 4) : 0;
+    w.total = at + 256;
+    return w;
+}
+
+// An operand as the products take it
+struct Rows {
+    const void *p;
+    int64_t ld;
+};
+
+struct Ffn {
+    const m3_ffn_dims *d;
+    FfnLayout w;
+    char *ws;
+    hipStream_t stream;
+    bool f32;
+    hipError_t e = hipSuccess;
+
+    Rows whole(const void *p, int64_t ld, int64_t rows, int64_t cols, int64_t padded, size_t at) {
+        const int64_t es = f32 ? 4 : 2;
+        if (padded == cols && ld * es % 16 == 0 && aligned(p, 16)) return Rows{p, ld};
+        if (e == hipSuccess && rows > 0) e = ffn::launch_pad(p, ld, ws + at, padded, rows, cols, f32, stream);
+        return Rows{ws + at, padded};
+    }
+    void gemm(const ffn::GemmArgs &g, bool at, bool bt, ffn::Kind kind, int batch) {
+        if (e == hipSuccess && g.M > 0 && g.N > 0) e = ffn::launch_gemm(g, f32, at, bt, kind, batch, stream);
+    }
+    ffn::GemmArgs args(int64_t M, int64_t N, int64_t K, Rows a, Rows b, void *c, int64_t ldc) const {
+        ffn::GemmArgs g = {};
+        g.a[0] = g.a[1] = a.p; g.b[0] = g.b[1] = b.p;
+        g.lda = a.ld; g.ldb = b.ld;
+        g.M = M; g.N = N; g.K = K; g.nseg = 1;
+        g.c[0] = g.c[1] = c; g.ldc = ldc;
+        g.gelu = d->act == M3_ACT_GELU;
+        return g;
+    }
+};
+
+}  // namespace
+
+extern "C" size_t m3_ffn_workspace_bytes(const m3_ffn_dims *d, int backward) {
+    return check_ffn(d, backward != 0) == M3_OK ? ffn_layout(d, backward != 0).total : 0;
+}
+
+static m3_status check_ffn_args(const m3_ffn_dims *d, const FfnLayout &w, const void *Wg, const void *Wu, const void *Wd,
+                                std::initializer_list<const void *> rest, const void *workspace, size_t workspace_bytes) {
+    if (!Wg || !Wu || !Wd) return M3_ERR_NULL;
+    const uintptr_t e = d->io == M3_F32 ? 4 : 2;
+    if (!aligned(Wg, w.pad_d ? e : 16) || !aligned(Wu, w.pad_d ? e : 16) || !aligned(Wd, w.pad_f ? e : 16)) return M3_ERR_ALIGN;
+    for (const void *p : rest)
+        if (!aligned(p, e)) return M3_ERR_ALIGN;
+    if (!workspace || workspace_bytes < w.total) return M3_ERR_WORKSPACE;
+    return aligned(workspace, 16) ? M3_OK : M3_ERR_ALIGN;
+}
+
+extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void *Wg, const void *Wu, const void *Wd,
+                                void *y, void *workspace, size_t workspace_bytes, void *stream) {
+    m3_status s = check_ffn(d, false);
+    if (s != M3_OK) return s;
+    const FfnLayout w = ffn_layout(d, false);
+    if (d->tokens > 0 && (!x || !y)) return M3_ERR_NULL;
+    s = check_ffn_args(d, w, Wg, Wu, Wd, {x, y}, workspace, workspace_bytes);
+    if (s != M3_OK || d->tokens == 0) return s;
+    const int64_t T = d->tokens, D = d->dmodel, F = d->dff;
+    Ffn f{d, w, static_cast<char *>(workspace), static_cast<hipStream_t>(stream), d->io == M3_F32};
+    const Rows rx = f.whole(x, d->x_stride, T, D, w.Dp, w.x);
+    const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
+    const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd), h{f.ws + w.h, w.Fp};
+    ffn::GemmArgs g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
+    g.b[1] = ru.p;
+    f.gemm(g, false, false, ffn::kGate, 1);
+    f.gemm(f.args(T, D, F, h, rd, y, D), false, false, ffn::kStore, 1);
+    return launched(f.e);
+}
+
+extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void *Wg, const void *Wu, const void *Wd,
+                                const void *dy, void *dx, void *dWg, void *dWu, void *dWd, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+    m3_status s = check_ffn(d, true);
+    if (s != M3_OK) return s;
+    const FfnLayout w = ffn_layout(d, true);
+    if (!dWg || !dWu || !dWd || (d->tokens > 0 && (!x || !dy || !dx))) return M3_ERR_NULL;
+    s = check_ffn_args(d, w, Wg, Wu, Wd, {x, dy, dx, dWg, dWu, dWd}, workspace, workspace_bytes);
+    if (s != M3_OK) return s;
+    const int64_t T = d->tokens, D = d->dmodel, F = d->dff;
+    Ffn f{d, w, static_cast<char *>(workspace), static_cast<hipStream_t>(stream), d->io == M3_F32};
+    const Rows rx = f.whole(x, d->x_stride, T, D, w.Dp, w.x), ry = f.whole(dy, d->dy_stride, T, D, w.Dp, w.dy);
+    const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
+    const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd);
+    const Rows h{f.ws + w.h, w.Fp}, dg{f.ws + w.dg, w.Fp}, du{f.ws + w.du, w.Fp};
+    // dh = dy Wd (with the padding's columns, zero, too)
+    f.gemm(f.args(T, w.Fp, D, ry, rd, f.ws + w.dh, w.Fp), false, true, ffn::kStoreF32, 1);
+    // g and u again; h, dg, du
+    ffn::GemmArgs g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
+    g.b[1] = ru.p;
+    g.dg = f.ws + w.dg; g.du = f.ws + w.du;
+    g.dh = reinterpret_cast<const float *>(f.ws + w.dh);
+    f.gemm(g, false, false, ffn::kGateBwd, 1);
+    // dx = dg Wg + du Wu
+    g = f.args(T, D, F, dg, rg, dx, D);
+    g.a[1] = du.p; g.b[1] = ru.p; g.nseg = 2;
+    f.gemm(g, false, true, ffn::kStore, 1);
+    // dWg = dg^T x, dWu = du^T x
+    g = f.args(F, D, T, dg, rx, dWg, D);
+    g.a[1] = du.p; g.c[1] = dWu;
+    f.gemm(g, true, true, ffn::kStore, 2);
+    f.gemm(f.args(D, F, T, ry, h, dWd, F), true, true, ffn::kStore, 1);
+    return launched(f.e);
 }
 
 // ---------------------------------------------------------------------------

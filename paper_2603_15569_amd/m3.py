@@ -55,6 +55,14 @@ class M3GlrDims(ctypes.Structure):
                 + [(f"{t}_stride_{a}", ctypes.c_int64) for t in "xriz" for a in "bt"])
 
 
+class M3FfnDims(ctypes.Structure):
+    """m3_ffn_dims: sizes, io dtype, activation and row strides of the feed-forward block."""
+    _fields_ = [("tokens", ctypes.c_int64), ("dmodel", ctypes.c_int64), ("dff", ctypes.c_int64),
+                ("io", ctypes.c_int32), ("act", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("dy_stride", ctypes.c_int64)]
+
+
+_ACT = {"silu": 0, "gelu": 1}   # M3_ACT_*
 GLR_CHUNK = 128             # M3_GLR_CHUNK: tokens between two saved states
 M3_ADAMW_8BIT = 1
 
@@ -83,7 +91,7 @@ EXPORTS = ("m3_scan_workspace_bytes", "m3_scan_fwd", "m3_scan_fwd_gated", "m3_sc
            "m3_step", "m3_step_gated", "m3_scan_check", "m3_set_wait_limit", "m3_scan_fwd_noalloc",
            "m3_scan_fwd_pro", "m3_step_pro", "m3_scan_bwd", "m3_scan_bwd_workspace_bytes",
            "m3_glr_workspace_bytes", "m3_glr_fwd", "m3_glr_bwd", "m3_glr_step", "m3_glr_check",
-           "m3_adamw_step",
+           "m3_ffn_workspace_bytes", "m3_ffn_fwd", "m3_ffn_bwd", "m3_adamw_step",
            "m3_status_string", "m3_last_hip_error")
 SCRATCH_BYTES = 256 << 20   # M3_SCRATCH_BYTES: the allocation-free scan's fixed workspace
 CTL_BYTES = 1280            # M3_CTL_BYTES: a scan workspace's control block (zero before first use)
@@ -138,9 +146,14 @@ def lib() -> ctypes.CDLL:
         L.m3_glr_bwd.argtypes = [glr_p] + [vp] * 14 + [vp, ctypes.c_size_t, vp]
         L.m3_glr_step.argtypes = [glr_p] + [vp] * 7 + [vp]
         L.m3_glr_check.argtypes = [glr_p, vp, ctypes.c_size_t, ctypes.POINTER(ctypes.c_uint32), vp]
+        ffn_p = ctypes.POINTER(M3FfnDims)
+        L.m3_ffn_workspace_bytes.argtypes = [ffn_p, ctypes.c_int]
+        L.m3_ffn_workspace_bytes.restype = ctypes.c_size_t
+        L.m3_ffn_fwd.argtypes = [ffn_p] + [vp] * 5 + [vp, ctypes.c_size_t, vp]
+        L.m3_ffn_bwd.argtypes = [ffn_p] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
         L.m3_adamw_step.argtypes = [ctypes.POINTER(M3AdamwConfig), ctypes.POINTER(M3AdamwTensor),
                                     ctypes.c_int64, vp, vp]
-        for name in ("glr_fwd", "glr_bwd", "glr_step", "glr_check", "adamw_step"):
+        for name in ("glr_fwd", "glr_bwd", "glr_step", "glr_check", "ffn_fwd", "ffn_bwd", "adamw_step"):
             getattr(L, "m3_" + name).restype = ctypes.c_int
         L.m3_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.m3_set_wait_limit.restype = None
@@ -662,6 +675,80 @@ def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
                              r.data_ptr(), i.data_ptr(), _f32(A, x.shape[1:], x.device, "A"),
                              None if z is None else z.data_ptr(), _p(y), _stream(stream)))
     return y
+
+
+# ---------------------------------------------------------------------------
+# Gated feed-forward block
+# ---------------------------------------------------------------------------
+
+def _ffn_rows(t: torch.Tensor, name: str) -> torch.Tensor:
+    """[..., D] as rows [T, D] (a view)."""
+    t = t if t.dim() == 2 else t.view(-1, t.shape[-1])
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
+    return t
+
+
+def _ffn_dims(x, Wg, act="silu", dy=None) -> M3FfnDims:
+    if x.dtype not in _IO:
+        raise ValueError("x must be fp32 or bf16")
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {sorted(_ACT)}")
+    T, D = x.shape
+    F = Wg.shape[0]
+    # (the stride of a single row is never walked, whatever torch reports)
+    st = [t.stride(0) if t is not None and T > 1 else D for t in (x, dy)]
+    return M3FfnDims(T, D, F, _IO[x.dtype], _ACT[act], *st)
+
+
+def ffn_workspace(x, Wg, backward: bool = False) -> torch.Tensor:
+    """A workspace for ffn_fwd (ffn_bwd with `backward`, which serves both) of x
+    [..., D] and Wg [F, D]: keep it for further calls, one at a time."""
+    d = _ffn_dims(_ffn_rows(x, "x"), Wg)
+    n = int(lib().m3_ffn_workspace_bytes(ctypes.byref(d), int(backward)))
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=x.device)
+
+
+def _ffn_check(x, Wg, Wu, Wd):
+    D, F = x.shape[-1], Wg.shape[0]
+    for name, t, shape in (("Wg", Wg, (F, D)), ("Wu", Wu, (F, D)), ("Wd", Wd, (D, F))):
+        if tuple(t.shape) != shape or t.dtype != x.dtype or t.device != x.device:
+            raise ValueError(f"{name} must be {x.dtype} {shape} on {x.device}")
+
+
+def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=None):
+    """m3_ffn_fwd: y = (act(x Wg^T) o (x Wu^T)) Wd^T; x [..., D] (rows of [T, D] may be
+    strided), Wg and Wu [F, D], Wd [D, F], bf16 or fp32; act "silu" or "gelu" (tanh
+    form).  Returns y, shaped like x."""
+    _ffn_check(x, Wg, Wu, Wd)
+    rows = _ffn_rows(x, "x")
+    d = _ffn_dims(rows, Wg, act)
+    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("y must have the shape and dtype of x")
+    if workspace is None:
+        workspace = ffn_workspace(x, Wg)
+    _check(lib().m3_ffn_fwd(ctypes.byref(d), rows.data_ptr(), _p(Wg), _p(Wu), _p(Wd), _p(y), _p(workspace),
+                            workspace.numel(), _stream(stream)))
+    return y
+
+
+def ffn_bwd(x, Wg, Wu, Wd, dy, act: str = "silu", workspace=None, stream=None):
+    """m3_ffn_bwd: gradients of J = <dy, y> from the forward's inputs (g and u are formed
+    again).  Returns a dict: dx (shaped like x), dWg, dWu, dWd, in the io dtype."""
+    _ffn_check(x, Wg, Wu, Wd)
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise ValueError("dy must have the shape and dtype of x")
+    rows, drows = _ffn_rows(x, "x"), _ffn_rows(dy, "dy")
+    d = _ffn_dims(rows, Wg, act, drows)
+    out = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device), dWg=torch.empty_like(Wg),
+               dWu=torch.empty_like(Wu), dWd=torch.empty_like(Wd))
+    if workspace is None:
+        workspace = ffn_workspace(x, Wg, backward=True)
+    _check(lib().m3_ffn_bwd(ctypes.byref(d), rows.data_ptr(), _p(Wg), _p(Wu), _p(Wd), drows.data_ptr(),
+                            _p(out["dx"]), _p(out["dWg"]), _p(out["dWu"]), _p(out["dWd"]), _p(workspace),
+                            workspace.numel(), _stream(stream)))
+    return out
 
 
 # ---------------------------------------------------------------------------
