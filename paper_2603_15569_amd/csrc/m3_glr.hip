@@ -33,6 +33,16 @@ __device__ __forceinline__ float get(uint16_t v, int) { return __uint_as_float((
 __device__ __forceinline__ float get(uint32_t v, int e) { return __uint_as_float(e ? v & 0xffff0000u : v << 16); }
 __device__ __forceinline__ float get(float v, int) { return v; }
 
+// Row access: a uniform pointer to the row and the lane's byte offset in it
+template <typename R> __device__ __forceinline__ R row_load(const void *row, uint32_t off) {
+    return *reinterpret_cast<const R *>(static_cast<const char *>(row) + off);
+}
+template <typename R> __device__ __forceinline__ void row_store(void *row, uint32_t off, R v) {
+    *reinterpret_cast<R *>(static_cast<char *>(row) + off) = v;
+}
+// Keeps the compiler from overlapping more tokens than registers are for.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
 // Makes a value unknown to the compiler, so that what is formed from it a
 // second time is formed again and not held in registers meanwhile.
 template <typename R> __device__ __forceinline__ void forget(R &v) { asm volatile("" : "+v"(v)); }
@@ -151,7 +161,7 @@ __device__ __forceinline__ void look_back(const Words &wd, int64_t slot0, int64_
         }
         __syncthreads();
         int at = -1;
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < NW; ++k) {
             const uint32_t kind = s_kind[k];
             if (kind == 2u) { at = k; break; }
@@ -160,6 +170,7 @@ __device__ __forceinline__ void look_back(const Words &wd, int64_t slot0, int64_
         if (at >= 0) {
 #pragma unroll
             for (int e = 0; e < V; ++e) enter[e] = s_val[at][0][lane * V + e];
+#pragma unroll 1
             for (int k = at - 1; k >= 0; --k)
 #pragma unroll
                 for (int e = 0; e < V; ++e)
@@ -197,16 +208,17 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
     const int n = (int)min((int64_t)S, a.L - t0);   // tokens of this wave, possibly none
 
     // rows past the end read the last token's (their maps are the identity)
-    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb + dl;
-    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb + dl;
-    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb + dl;
+    const uint32_t lo = (uint32_t)(dl * sizeof(T));
+    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb;
+    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb;
+    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb;
     R vx[S], vr[S], vi[S], vz[kGate ? S : 1];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         const int64_t t = min(t0 + s, a.L - 1);
-        vr[s] = *reinterpret_cast<const R *>(pr + t * a.r_st);
-        vi[s] = *reinterpret_cast<const R *>(pi + t * a.i_st);
-        vx[s] = *reinterpret_cast<const R *>(px + t * a.x_st);
+        vr[s] = row_load<R>(pr + t * a.r_st, lo);
+        vi[s] = row_load<R>(pi + t * a.i_st, lo);
+        vx[s] = row_load<R>(px + t * a.x_st, lo);
     }
     float A[V];
 #pragma unroll
@@ -229,11 +241,12 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
             pa[s][e] = ca[e];
             ph[s][e] = ch[e];
         }
+        fence();
     }
     if constexpr (kGate) {
-        const T *pz = static_cast<const T *>(a.z) + it.b * a.z_sb + dl;
+        const T *pz = static_cast<const T *>(a.z) + it.b * a.z_sb;
 #pragma unroll
-        for (int s = 0; s < S; ++s) vz[s] = *reinterpret_cast<const R *>(pz + min(t0 + s, a.L - 1) * a.z_st);
+        for (int s = 0; s < S; ++s) vz[s] = row_load<R>(pz + min(t0 + s, a.L - 1) * a.z_st, lo);
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -245,7 +258,7 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
     float wA[V], wc[V], tA[V], tc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { wA[e] = 1.f; wc[e] = 0.f; tA[e] = 1.f; tc[e] = 0.f; }
-#pragma unroll
+#pragma unroll 4
     for (int k = 0; k < NW; ++k) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -285,17 +298,17 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
     float hw[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) hw[e] = after(wA[e], enter[e], wc[e]);
-    T *py = static_cast<T *>(a.y) + (it.b * a.L + t0) * a.D + d0;
+    T *py = static_cast<T *>(a.y) + (it.b * a.L + t0) * a.D;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        if (s >= n) break;
+        if (s >= n) continue;
         float o[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             o[e] = fmaf(pa[s][e], hw[e], ph[s][e]);
             if constexpr (kGate) o[e] *= silu(get(vz[s], e));
         }
-        *reinterpret_cast<R *>(py + s * a.D) = put<T, V>(o);
+        row_store<R>(py + s * a.D, lo, put<T, V>(o));
     }
 }
 
@@ -324,20 +337,20 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     const int64_t t0 = tile * kChunk + wave * S;
     const int n = (int)min((int64_t)S, a.L - t0);
 
-    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb + dl;
-    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb + dl;
-    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb + dl;
-    const T *pd = static_cast<const T *>(a.dy) + it.b * a.L * a.D + dl;
+    const uint32_t lo = (uint32_t)(dl * sizeof(T));
+    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb;
+    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb;
+    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb;
+    const T *pd = static_cast<const T *>(a.dy) + it.b * a.L * a.D;
     R vx[S], vr[S], vi[S], vd[S], vz[kGate ? S : 1];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         const int64_t t = min(t0 + s, a.L - 1);
-        vr[s] = *reinterpret_cast<const R *>(pr + t * a.r_st);
-        vi[s] = *reinterpret_cast<const R *>(pi + t * a.i_st);
-        vx[s] = *reinterpret_cast<const R *>(px + t * a.x_st);
-        vd[s] = *reinterpret_cast<const R *>(pd + t * a.D);
-        if constexpr (kGate)
-            vz[s] = *reinterpret_cast<const R *>(static_cast<const T *>(a.z) + it.b * a.z_sb + dl + t * a.z_st);
+        vr[s] = row_load<R>(pr + t * a.r_st, lo);
+        vi[s] = row_load<R>(pi + t * a.i_st, lo);
+        vx[s] = row_load<R>(px + t * a.x_st, lo);
+        vd[s] = row_load<R>(pd + t * a.D, lo);
+        if constexpr (kGate) vz[s] = row_load<R>(static_cast<const T *>(a.z) + it.b * a.z_sb + t * a.z_st, lo);
     }
     float A[V], enter[V];
     const int64_t srow = (it.b * a.tiles + tile) * a.D;
@@ -363,6 +376,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
             cA[e] *= at[s][e];
             cc[e] = fmaf(at[s][e], cc[e], bt[s][e]);
         }
+        fence();
     }
 #pragma unroll
     for (int s = S - 1; s >= 0; --s) {
@@ -372,6 +386,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
             if constexpr (kGate) dh *= silu(get(vz[s], e));
             cq[e] = s < n ? at[s][e] * (dh + cq[e]) : cq[e];
         }
+        fence();
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -383,10 +398,11 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     float h[V], tA[V], tq[V], wA[V], wq[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { h[e] = enter[e]; tA[e] = 1.f; tq[e] = 0.f; wA[e] = 1.f; wq[e] = 0.f; }
+#pragma unroll 1
     for (int k = 0; k < wave; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) h[e] = fmaf(s_A[k][lane * V + e], h[e], s_c[k][lane * V + e]);
-#pragma unroll
+#pragma unroll 4
     for (int k = NW - 1; k >= 0; --k) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -434,12 +450,14 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     float dA[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { q[e] = after(wA[e], q[e], wq[e]); dA[e] = 0.f; }
-    const int64_t orow = (it.b * a.L + t0) * a.D + dl;
+    const int64_t orow = (it.b * a.L + t0) * a.D;
 #pragma unroll
     for (int s = S - 1; s >= 0; --s) {
         if (s >= n) continue;
         forget(vr[s]);
         forget(vi[s]);
+        forget(vx[s]);
+        forget(vd[s]);
         float ox[V], orr[V], oi[V], oz[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -465,11 +483,12 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
             dA[e] += rd;
         }
         if (live) {
-            *reinterpret_cast<R *>(static_cast<T *>(a.dx) + orow + s * a.D) = put<T, V>(ox);
-            *reinterpret_cast<R *>(static_cast<T *>(a.dr) + orow + s * a.D) = put<T, V>(orr);
-            *reinterpret_cast<R *>(static_cast<T *>(a.di) + orow + s * a.D) = put<T, V>(oi);
-            if constexpr (kGate) *reinterpret_cast<R *>(static_cast<T *>(a.dz) + orow + s * a.D) = put<T, V>(oz);
+            row_store<R>(static_cast<T *>(a.dx) + orow + s * a.D, lo, put<T, V>(ox));
+            row_store<R>(static_cast<T *>(a.dr) + orow + s * a.D, lo, put<T, V>(orr));
+            row_store<R>(static_cast<T *>(a.di) + orow + s * a.D, lo, put<T, V>(oi));
+            if constexpr (kGate) row_store<R>(static_cast<T *>(a.dz) + orow + s * a.D, lo, put<T, V>(oz));
         }
+        fence();
     }
     // the tile's part of dA (tagged like every word of the workspace)
     __syncthreads();
@@ -480,7 +499,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             float sum = 0.f;
-#pragma unroll
+#pragma unroll 4
             for (int k = 0; k < NW; ++k) sum += s_c[k][lane * V + e];
             a.part[(it.b * a.tiles + tile) * a.D + d0 + e] = (uint64_t)__float_as_uint(sum);
         }
