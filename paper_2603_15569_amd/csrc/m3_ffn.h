@@ -32,6 +32,20 @@ enum Kind {
     kGateBwd,    // h, dg, du from g, u and dh
 };
 
+// A few rows of x (T of them) times many rows of weights: out[t][r] = sum over
+// k of x(t, k) w(r, k), or the two gates with w[0] = Wg and w[1] = Wu.
+constexpr int kFewRows = 64;
+struct FewArgs {
+    const void *x, *w[2];
+    int64_t ldx, ldw;      // elements; rows start on 16 bytes
+    int64_t T, R, K;       // K: whole 16-byte pieces
+    int64_t Ro;            // columns of out: R and any padding, written as zeros
+    void *out;
+    int64_t ldo;
+    int gelu;
+};
+hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s);
+
 // C = A B (both as [row][k], or B or both turned), the two gates
 hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s);
 // rows of `cols` elements copied to rows of `ld`, zeros after

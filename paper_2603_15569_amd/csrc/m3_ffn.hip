@@ -336,6 +336,117 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     }
 }
 
+// Few rows of x: bound by reading the weights once.  A workgroup takes RH rows
+// of weights (of both gates), its waves interleaved pieces of k, 256 bytes of
+// every row at a time; the weights are the MFMA's row operand straight from
+// global memory, x (read again by every workgroup, from the caches) its
+// columns, 16 a tile.  The waves' sums meet in LDS.  RH = 8 (half of the MFMA
+// rows repeat the others, at the same addresses) where 16 would leave compute
+// units without work.
+template <typename T, int TT, int RH, int NW, bool kGates>
+__global__ __launch_bounds__(NW * 64) void k_few(FewArgs a) {
+    constexpr int EL = 16 / sizeof(T), KS = 4 * EL, U = 4, NM = kGates ? 2 : 1;
+    __shared__ f32x4 s_acc[NW][NM * TT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int l16 = lane & 15, q = lane / 16;
+    const int64_t r0 = (int64_t)blockIdx.x * RH;
+    const Rsrc rx = make_rsrc(a.x, span<T>(a.T, a.ldx, a.K, kFewRows));
+    Rsrc rw[NM];
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+        rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>(a.R - r0, a.ldw, a.K, RH));
+    const uint32_t wo = (uint32_t)((l16 & (RH - 1)) * (int)(a.ldw * sizeof(T)) + q * 16);
+    const uint32_t xo = (uint32_t)(l16 * (int)(a.ldx * sizeof(T)) + q * 16);
+    const uint32_t xt = (uint32_t)(16 * (int)(a.ldx * sizeof(T)));
+    const int K = (int)a.K, units = (K + U * KS - 1) / (U * KS);
+
+    f32x4 acc[NM][TT];
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 w[U][NM];
+    auto load_w = [&](int unit) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = (unit * U + u) * KS;
+            const bool in = k + q * EL < K;
+#pragma unroll
+            for (int m = 0; m < NM; ++m) w[u][m] = scan::buf_load<f32x4>(rw[m], in ? wo + (uint32_t)(k * (int)sizeof(T)) : kOut);
+        }
+    };
+    if (wave < units) load_w(wave);
+    for (int unit = wave; unit < units; unit += NW) {
+        f32x4 x[U][TT], v[U][NM];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = (unit * U + u) * KS;
+            const bool in = k + q * EL < K;
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+                x[u][t] = scan::buf_load<f32x4>(rx, in ? xo + t * xt + (uint32_t)(k * (int)sizeof(T)) : kOut);
+#pragma unroll
+            for (int m = 0; m < NM; ++m) v[u][m] = w[u][m];
+        }
+        if (unit + NW < units) load_w(unit + NW);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int m = 0; m < NM; ++m) acc[m][t] = mma<T>(v[u][m], x[u][t], acc[m][t]);
+    }
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) s_acc[wave][m * TT + t][lane] = acc[m][t];
+    __syncthreads();
+    // rows 4 q .. 4 q + 3 of the weights, row l16 of x's tile
+    for (int k = threadIdx.x; k < TT * 64; k += NW * 64) {
+        const int t = k / 64, ln = k % 64, row = ln / 16 * 4;
+        f32x4 sum[NM];
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            sum[m] = s_acc[0][m * TT + t][ln];
+            for (int v = 1; v < NW; ++v) sum[m] += s_acc[v][m * TT + t][ln];
+        }
+        const int64_t col = t * 16 + ln % 16, r = r0 + row;
+        if (row >= RH || col >= a.T || r >= a.Ro) continue;
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] = sum[0][e];
+            if constexpr (kGates) {
+                float slope;
+                o[e] = act(sum[0][e], a.gelu != 0, slope) * sum[NM - 1][e];
+            }
+        }
+        T *dst = static_cast<T *>(a.out) + col * a.ldo + r;
+        if (r + 4 <= a.Ro && a.ldo * sizeof(T) % 16 == 0 && ((uintptr_t)a.out & 15) == 0) {
+            scan::store4(dst, f32x4{o[0], o[1], o[2], o[3]});
+        } else {
+            for (int e = 0; e < 4; ++e)
+                if (r + e < a.Ro) dst[e] = (T)o[e];
+        }
+    }
+}
+
+template <typename T, int TT, bool kGates> hipError_t few(const FewArgs &a, hipStream_t s) {
+    // 16 rows a workgroup where that makes two for every compute unit, else 8
+    const int64_t wide = (a.Ro + 15) / 16;
+    if (wide >= 512) k_few<T, TT, 16, 8, kGates><<<dim3((unsigned)wide), dim3(512), 0, s>>>(a);
+    else k_few<T, TT, 8, 8, kGates><<<dim3((unsigned)((a.Ro + 7) / 8)), dim3(512), 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, bool kGates> hipError_t few_rows(const FewArgs &a, hipStream_t s) {
+    switch ((a.T + 15) / 16) {
+    case 1: return few<T, 1, kGates>(a, s);
+    case 2: return few<T, 2, kGates>(a, s);
+    case 3: return few<T, 3, kGates>(a, s);
+    default: return few<T, 4, kGates>(a, s);
+    }
+}
+
 template <typename T> __global__ __launch_bounds__(256) void k_pad(const T *src, int64_t src_ld, T *dst, int64_t dst_ld,
                                                                     int64_t cols) {
     const int64_t row = blockIdx.x;
@@ -370,6 +481,10 @@ template <typename T> hipError_t dispatch(const GemmArgs &g, bool at, bool bt, K
 
 hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s) {
     return f32 ? dispatch<float>(g, at, bt, kind, batch, s) : dispatch<bf16>(g, at, bt, kind, batch, s);
+}
+hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s) {
+    if (f32) return gates ? few_rows<float, true>(a, s) : few_rows<float, false>(a, s);
+    return gates ? few_rows<bf16, true>(a, s) : few_rows<bf16, false>(a, s);
 }
 hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
                       hipStream_t s) {

@@ -302,6 +302,14 @@ extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rx = f.whole(x, d->x_stride, T, D, w.Dp, w.x);
     const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd), h{f.ws + w.h, w.Fp};
+    if (T <= ffn::kFewRows && f.e == hipSuccess) {
+        // (K in whole pieces: the copies are padded with zeros, and so is h)
+        ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU};
+        f.e = ffn::launch_few(a, f.f32, true, f.stream);
+        a = ffn::FewArgs{h.p, {rd.p, rd.p}, h.ld, rd.ld, T, D, w.Fp, D, y, D, 0};
+        if (f.e == hipSuccess) f.e = ffn::launch_few(a, f.f32, false, f.stream);
+        return launched(f.e);
+    }
     ffn::GemmArgs g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
     g.b[1] = ru.p;
     f.gemm(g, false, false, ffn::kGate, 1);
