@@ -571,8 +571,8 @@ m3_status m3_glr_check(const m3_glr_dims *dims, const void *workspace, size_t wo
  * initialisation (0 on invalid dims).  Rows that do not start on 16 bytes (odd
  * sizes or strides) are first copied there to rows that do.  Deterministic.
  * Alignment: the workspace 16 bytes; weights 16 bytes where their rows are
- * whole 16-byte pieces; else the element's (else M3_ERR_ALIGN).  dmodel, dff
- * and the strides are at most 2^20.  Outputs must not overlap inputs.
+ * whole 16-byte pieces; else the element's (else M3_ERR_ALIGN).  dmodel and
+ * dff are at most 2^16, the strides 2^20.  Outputs must not overlap inputs.
  */
 #define M3_ACT_SILU 0
 #define M3_ACT_GELU 1

@@ -12,25 +12,38 @@ namespace ffn {
 // next to each other ([m][k]) or with its own axis so ([k][m], "turned").
 // Rows start on 16 bytes.
 struct GemmArgs {
-    const void *a[2], *b[2];   // two: two products summed (nseg), two products (grid z), or the two gates (b)
+    const void *a[2], *b[2];   // two: two products summed (nseg), two products (batch), or the two gates (b)
     int64_t lda, ldb;          // elements
     int64_t M, N, K;
-    int nseg;
+    int nseg, batch;
     void *c[2];
     int64_t ldc;
+    int f32_out;               // c is fp32 whatever the io dtype
     // gates: h, dg, du with rows of ldc elements (columns N .. ldc - 1 are written as zeros), dh in fp32
     void *dg, *du;
     const float *dh;
     int gelu;
-    int tiles_m, tiles_n;
+    // set at launch: tiles, and the parts that k is split into (their sums go
+    // to `part`, [product][split][M][part_ld], and are joined there)
+    int tiles_m, tiles_n, splits;
+    float *part;
+    int64_t part_ld;
 };
 
 enum Kind {
-    kStore,      // C in the io dtype
-    kStoreF32,   // C in fp32
+    kStore,      // C
     kGate,       // h = act(g) u
     kGateBwd,    // h, dg, du from g, u and dh
 };
+
+// Room for the parts of split products, and the few rows' (below).
+constexpr size_t kPartBytes = (size_t)32 << 20;
+
+// C = A B (both as [row][k], or B or both turned), the two gates
+hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, hipStream_t s);
+// rows of `cols` elements copied to rows of `ld`, zeros after
+hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
+                      hipStream_t s);
 
 // A few rows of x (T of them) times many rows of weights: out[t][r] = sum over
 // k of x(t, k) w(r, k), or the two gates with w[0] = Wg and w[1] = Wu.
@@ -43,14 +56,10 @@ struct FewArgs {
     void *out;
     int64_t ldo;
     int gelu;
+    float *part;           // kPartBytes
+    int splits;            // set at launch
 };
 hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s);
-
-// C = A B (both as [row][k], or B or both turned), the two gates
-hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s);
-// rows of `cols` elements copied to rows of `ld`, zeros after
-hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
-                      hipStream_t s);
 
 }  // namespace ffn
 }  // namespace m3

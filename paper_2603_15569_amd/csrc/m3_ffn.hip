@@ -11,6 +11,8 @@
 //
 // Edges: buffer loads return zero past the end of an operand, so rows past M,
 // N or (turned) K need no masks; k past K within a row is sent out of range.
+#include <algorithm>
+
 #include "m3_device.h"
 #include "m3_ffn.h"
 #include "m3_scan_common.h"
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     const int grp = t / (GM * g.tiles_n), in = t % (GM * g.tiles_n);
     const int gm = min(GM, g.tiles_m - grp * GM);
     const int64_t m0 = (int64_t)(grp * GM + in % gm) * BM, n0 = (int64_t)(in / gm) * NB;
-    const int z = (int)blockIdx.z;
+    const int z = (int)blockIdx.z / g.splits, split = (int)blockIdx.z % g.splits;
 
     Tile<T, BM, NW, kAT, false> ta;
     Tile<T, BN, NW, kBT, kPair> tb;
@@ -173,6 +175,7 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     }
 
     const int nk = (int)((g.K + BK - 1) / BK), steps = nk * g.nseg;
+    const int it0 = (int)((int64_t)steps * split / g.splits), it1 = (int)((int64_t)steps * (split + 1) / g.splits);
     auto load = [&](int it) {
         const int seg = it >= nk ? 1 : 0;
         const int64_t k0 = (int64_t)(it - seg * nk) * BK;
@@ -219,11 +222,11 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    if (steps > 0) load(0);
-    for (int it = 0; it < steps; ++it) {
+    if (it0 < it1) load(it0);
+    for (int it = it0; it < it1; ++it) {
         __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's pieces of the stage have landed (vmcnt 0)
         __syncthreads();                      // everyone's have, and the other stage has been read
-        if (it + 1 < steps) load(it + 1);
+        if (it + 1 < it1) load(it + 1);
         const char *sa = lds[it & 1], *sb = sa + BM * kRowBytes;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -299,53 +302,86 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
             }
         }
     } else {
-        typedef typename std::conditional<KIND == kStoreF32, float, T>::type O;
-        O *c = static_cast<O *>(g.c[z]);
         constexpr int RUN = kPair ? 8 : 4;         // columns in a row a lane
-        const bool whole = g.ldc * sizeof(O) % 16 == 0 && ((uintptr_t)c & 15) == 0;
+        // (c or a part, in fp32 or the io dtype)
+        auto store = [&](auto *c, int64_t ldc, int64_t cols) {
+            typedef typename std::remove_pointer<decltype(c)>::type O;
+            const bool whole = ldc * sizeof(O) % 16 == 0 && ((uintptr_t)c & 15) == 0;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t m = mw + 16 * i + l16;
-            if (m >= g.M) continue;
+            for (int i = 0; i < MT; ++i) {
+                const int64_t m = mw + 16 * i + l16;
+                if (m >= g.M) continue;
 #pragma unroll
-            for (int p = 0; p < NT; p += RUN / 4) {
-                const int64_t n = n0 + wn * WN + (kPair ? p / 2 * 32 + 8 * q : 16 * p + 4 * q);
-                if (n >= g.N) continue;
-                float v[RUN];
+                for (int p = 0; p < NT; p += RUN / 4) {
+                    const int64_t n = n0 + wn * WN + (kPair ? p / 2 * 32 + 8 * q : 16 * p + 4 * q);
+                    if (n >= cols) continue;
+                    float v[RUN];
 #pragma unroll
-                for (int e = 0; e < RUN; ++e) v[e] = acc[i][p + e / 4][e % 4];
-                O *o = c + m * g.ldc + n;
-                if (whole && n + RUN <= g.N) {
-                    if constexpr (sizeof(O) == 4) {
+                    for (int e = 0; e < RUN; ++e) v[e] = acc[i][p + e / 4][e % 4];
+                    O *o = c + m * ldc + n;
+                    if (whole && n + RUN <= cols) {
+                        if constexpr (sizeof(O) == 4) {
 #pragma unroll
-                        for (int e = 0; e < RUN; e += 4) *reinterpret_cast<f32x4 *>(o + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                            for (int e = 0; e < RUN; e += 4)
+                                *reinterpret_cast<f32x4 *>(o + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                        } else {
+                            typedef __bf16 piece __attribute__((ext_vector_type(RUN)));
+                            piece w;
+#pragma unroll
+                            for (int e = 0; e < RUN; ++e) w[e] = (bf16)v[e];
+                            *reinterpret_cast<piece *>(o) = w;
+                        }
                     } else {
-                        typedef __bf16 piece __attribute__((ext_vector_type(RUN)));
-                        piece w;
 #pragma unroll
-                        for (int e = 0; e < RUN; ++e) w[e] = (bf16)v[e];
-                        *reinterpret_cast<piece *>(o) = w;
+                        for (int e = 0; e < RUN; ++e)
+                            if (n + e < cols) o[e] = (O)v[e];
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < RUN; ++e)
-                        if (n + e < g.N) o[e] = (O)v[e];
                 }
             }
-        }
+        };
+        if (g.splits > 1) store(g.part + (int64_t)blockIdx.z * g.M * g.part_ld, g.part_ld, g.part_ld);
+        else if (g.f32_out) store(static_cast<float *>(g.c[z]), g.ldc, g.N);
+        else store(static_cast<T *>(g.c[z]), g.ldc, g.N);
     }
 }
 
-// Few rows of x: bound by reading the weights once.  A workgroup takes RH rows
-// of weights (of both gates), its waves interleaved pieces of k, 256 bytes of
-// every row at a time; the weights are the MFMA's row operand straight from
+// Sums of a product's parts, in order, to the io dtype or fp32: four columns a thread.
+template <typename O> __global__ __launch_bounds__(256) void k_join(const float *part, int64_t ld, int splits, int64_t M, int64_t N,
+                                                                   O *c0, O *c1, int64_t ldc) {
+    const int64_t per = ld / 4, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (k >= M * per) return;
+    const int64_t m = k / per, n = k % per * 4;
+    const float *p = part + ((int64_t)blockIdx.y * splits * M + m) * ld + n;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4 *>(p + s * M * ld);
+    O *o = (blockIdx.y ? c1 : c0) + m * ldc + n;
+    if (n + 4 <= N && ldc % 4 == 0 && ((uintptr_t)o & (4 * sizeof(O) - 1)) == 0) {
+        scan::store4(o, v);
+    } else {
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) o[e] = (O)v[e];
+    }
+}
+hipError_t join(const float *part, int64_t ld, int splits, int64_t M, int64_t N, void *c0, void *c1, int batch, int64_t ldc,
+                bool f32, hipStream_t s) {
+    const dim3 grid((unsigned)((M * (ld / 4) + 255) / 256), (unsigned)batch), block(256);
+    if (f32) k_join<float><<<grid, block, 0, s>>>(part, ld, splits, M, N, static_cast<float *>(c0), static_cast<float *>(c1), ldc);
+    else k_join<bf16><<<grid, block, 0, s>>>(part, ld, splits, M, N, static_cast<bf16 *>(c0), static_cast<bf16 *>(c1), ldc);
+    return hipGetLastError();
+}
+
+// Few rows of x: bound by reading the weights once.  A workgroup takes 16 RT
+// rows of weights (of both gates), its waves interleaved pieces of k, U runs of
+// 64 bytes of every row at a time; the weights are the MFMA's row operand straight from
 // global memory, x (read again by every workgroup, from the caches) its
-// columns, 16 a tile.  The waves' sums meet in LDS.  RH = 8 (half of the MFMA
-// rows repeat the others, at the same addresses) where 16 would leave compute
-// units without work.
-template <typename T, int TT, int RH, int NW, bool kGates>
-__global__ __launch_bounds__(NW * 64) void k_few(FewArgs a) {
-    constexpr int EL = 16 / sizeof(T), KS = 4 * EL, U = 4, NM = kGates ? 2 : 1;
+// columns, 16 a tile.  The waves' sums meet in LDS.  Without gates k is also
+// split over workgroups (the parts joined after), so that few rows of weights
+// fill the device while a workgroup has enough of them: reading x again costs
+// as many bytes a workgroup as its weights when it has T rows of them.
+template <typename T, int TT, int RT, bool kGates>
+__global__ __launch_bounds__(512) void k_few(FewArgs a) {
+    constexpr int NW = 8, NM = kGates ? 2 : 1, U = NM * RT * TT >= 8 ? 2 : 4;
+    constexpr int EL = 16 / sizeof(T), KS = 4 * EL, RH = 16 * RT;
     __shared__ f32x4 s_acc[NW][NM * TT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int l16 = lane & 15, q = lane / 16;
@@ -355,29 +391,34 @@ __global__ __launch_bounds__(NW * 64) void k_few(FewArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m)
         rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>(a.R - r0, a.ldw, a.K, RH));
-    const uint32_t wo = (uint32_t)((l16 & (RH - 1)) * (int)(a.ldw * sizeof(T)) + q * 16);
-    const uint32_t xo = (uint32_t)(l16 * (int)(a.ldx * sizeof(T)) + q * 16);
-    const uint32_t xt = (uint32_t)(16 * (int)(a.ldx * sizeof(T)));
-    const int K = (int)a.K, units = (K + U * KS - 1) / (U * KS);
+    const uint32_t wo = (uint32_t)(l16 * (int)(a.ldw * sizeof(T)) + q * 16), wt = (uint32_t)(16 * (int)(a.ldw * sizeof(T)));
+    const uint32_t xo = (uint32_t)(l16 * (int)(a.ldx * sizeof(T)) + q * 16), xt = (uint32_t)(16 * (int)(a.ldx * sizeof(T)));
+    const int K = (int)a.K, all = (K + U * KS - 1) / (U * KS), split = (int)blockIdx.y;
+    const int u0 = (int)((int64_t)all * split / a.splits), u1 = (int)((int64_t)all * (split + 1) / a.splits);
 
-    f32x4 acc[NM][TT];
+    f32x4 acc[RT][NM][TT];
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int t = 0; t < TT; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    f32x4 w[U][NM];
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) acc[i][m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 w[U][RT][NM];
     auto load_w = [&](int unit) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = (unit * U + u) * KS;
             const bool in = k + q * EL < K;
 #pragma unroll
-            for (int m = 0; m < NM; ++m) w[u][m] = scan::buf_load<f32x4>(rw[m], in ? wo + (uint32_t)(k * (int)sizeof(T)) : kOut);
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int m = 0; m < NM; ++m)
+                    w[u][i][m] = scan::buf_load<f32x4>(rw[m], in ? wo + i * wt + (uint32_t)(k * (int)sizeof(T)) : kOut);
         }
     };
-    if (wave < units) load_w(wave);
-    for (int unit = wave; unit < units; unit += NW) {
-        f32x4 x[U][TT], v[U][NM];
+    if (u0 + wave < u1) load_w(u0 + wave);
+    for (int unit = u0 + wave; unit < u1; unit += NW) {
+        f32x4 x[U][TT], v[U][RT][NM];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = (unit * U + u) * KS;
@@ -386,57 +427,84 @@ __global__ __launch_bounds__(NW * 64) void k_few(FewArgs a) {
             for (int t = 0; t < TT; ++t)
                 x[u][t] = scan::buf_load<f32x4>(rx, in ? xo + t * xt + (uint32_t)(k * (int)sizeof(T)) : kOut);
 #pragma unroll
-            for (int m = 0; m < NM; ++m) v[u][m] = w[u][m];
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int m = 0; m < NM; ++m) v[u][i][m] = w[u][i][m];
         }
-        if (unit + NW < units) load_w(unit + NW);
+        if (unit + NW < u1) load_w(unit + NW);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int t = 0; t < TT; ++t)
 #pragma unroll
-                for (int m = 0; m < NM; ++m) acc[m][t] = mma<T>(v[u][m], x[u][t], acc[m][t]);
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int m = 0; m < NM; ++m) acc[i][m][t] = mma<T>(v[u][i][m], x[u][t], acc[i][m][t]);
     }
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+    for (int i = 0; i < RT; ++i) {
+        if (i) __syncthreads();
 #pragma unroll
-        for (int t = 0; t < TT; ++t) s_acc[wave][m * TT + t][lane] = acc[m][t];
-    __syncthreads();
-    // rows 4 q .. 4 q + 3 of the weights, row l16 of x's tile
-    for (int k = threadIdx.x; k < TT * 64; k += NW * 64) {
-        const int t = k / 64, ln = k % 64, row = ln / 16 * 4;
-        f32x4 sum[NM];
+        for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int m = 0; m < NM; ++m) {
-            sum[m] = s_acc[0][m * TT + t][ln];
-            for (int v = 1; v < NW; ++v) sum[m] += s_acc[v][m * TT + t][ln];
-        }
-        const int64_t col = t * 16 + ln % 16, r = r0 + row;
-        if (row >= RH || col >= a.T || r >= a.Ro) continue;
-        float o[4];
+            for (int t = 0; t < TT; ++t) s_acc[wave][m * TT + t][lane] = acc[i][m][t];
+        __syncthreads();
+        // rows 4 q .. 4 q + 3 of the weights' tile, row l16 of x's
+        for (int k = threadIdx.x; k < TT * 64; k += NW * 64) {
+            const int t = k / 64, ln = k % 64;
+            f32x4 sum[NM];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = sum[0][e];
-            if constexpr (kGates) {
-                float slope;
-                o[e] = act(sum[0][e], a.gelu != 0, slope) * sum[NM - 1][e];
+            for (int m = 0; m < NM; ++m) {
+                sum[m] = s_acc[0][m * TT + t][ln];
+                for (int v = 1; v < NW; ++v) sum[m] += s_acc[v][m * TT + t][ln];
             }
-        }
-        T *dst = static_cast<T *>(a.out) + col * a.ldo + r;
-        if (r + 4 <= a.Ro && a.ldo * sizeof(T) % 16 == 0 && ((uintptr_t)a.out & 15) == 0) {
-            scan::store4(dst, f32x4{o[0], o[1], o[2], o[3]});
-        } else {
-            for (int e = 0; e < 4; ++e)
-                if (r + e < a.Ro) dst[e] = (T)o[e];
+            const int64_t col = t * 16 + ln % 16, r = r0 + 16 * i + ln / 16 * 4;
+            if (col >= a.T || r >= a.Ro) continue;
+            if (!kGates && a.splits > 1) {   // (rows of whole fours)
+                const int64_t ld = (a.Ro + 3) / 4 * 4;
+                *reinterpret_cast<f32x4 *>(a.part + ((int64_t)split * a.T + col) * ld + r) = sum[0];
+                continue;
+            }
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[e] = sum[0][e];
+                if constexpr (kGates) {
+                    float slope;
+                    o[e] = act(sum[0][e], a.gelu != 0, slope) * sum[NM - 1][e];
+                }
+            }
+            T *dst = static_cast<T *>(a.out) + col * a.ldo + r;
+            if (r + 4 <= a.Ro && a.ldo * sizeof(T) % 16 == 0 && ((uintptr_t)a.out & 15) == 0) {
+                scan::store4(dst, f32x4{o[0], o[1], o[2], o[3]});
+            } else {
+                for (int e = 0; e < 4; ++e)
+                    if (r + e < a.Ro) dst[e] = (T)o[e];
+            }
         }
     }
 }
 
+template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a, int splits, hipStream_t s) {
+    a.splits = splits;
+    k_few<T, TT, RT, kGates><<<dim3((unsigned)((a.Ro + 16 * RT - 1) / (16 * RT)), (unsigned)splits), dim3(512), 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    return join(a.part, (a.Ro + 3) / 4 * 4, splits, a.T, a.Ro, a.out, a.out, 1, a.ldo, sizeof(T) == 4, s);
+}
 template <typename T, int TT, bool kGates> hipError_t few(const FewArgs &a, hipStream_t s) {
-    // 16 rows a workgroup where that makes two for every compute unit, else 8
-    const int64_t wide = (a.Ro + 15) / 16;
-    if (wide >= 512) k_few<T, TT, 16, 8, kGates><<<dim3((unsigned)wide), dim3(512), 0, s>>>(a);
-    else k_few<T, TT, 8, 8, kGates><<<dim3((unsigned)((a.Ro + 7) / 8)), dim3(512), 0, s>>>(a);
-    return hipGetLastError();
+    // 32 rows a workgroup where there are enough for every compute unit, and
+    // where k can be split
+    const int64_t wide = (a.Ro + 31) / 32;
+    if constexpr (kGates) {
+        return TT > 1 && wide >= 256 ? few_run<T, TT, 2, true>(a, 1, s) : few_run<T, TT, 1, true>(a, 1, s);
+    } else {
+        const int64_t groups = TT > 1 ? wide : (a.Ro + 15) / 16;
+        // parts of at least 1 KiB of each row for each of the waves
+        const int64_t most = std::min<int64_t>(8, a.K * (int64_t)sizeof(T) / 4096);
+        const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / groups));
+        return TT > 1 ? few_run<T, TT, 2, false>(a, splits, s) : few_run<T, TT, 1, false>(a, splits, s);
+    }
 }
 template <typename T, bool kGates> hipError_t few_rows(const FewArgs &a, hipStream_t s) {
     switch ((a.T + 15) / 16) {
@@ -454,33 +522,66 @@ template <typename T> __global__ __launch_bounds__(256) void k_pad(const T *src,
 }
 
 template <typename T, int BM, int BN, int NWM, int NWN, bool kAT, bool kBT, Kind KIND>
-hipError_t run(GemmArgs g, int batch, hipStream_t s) {
-    constexpr int NB = KIND == kGate || KIND == kGateBwd ? BN / 2 : BN;
-    const int64_t n = KIND == kGate || KIND == kGateBwd ? g.ldc : g.N;
+hipError_t run(GemmArgs g, int splits, hipStream_t s) {
+    constexpr bool kGates = KIND == kGate || KIND == kGateBwd;
+    constexpr int NB = kGates ? BN / 2 : BN;
     g.tiles_m = (int)((g.M + BM - 1) / BM);
-    g.tiles_n = (int)((n + NB - 1) / NB);
+    g.tiles_n = (int)(((kGates ? g.ldc : g.N) + NB - 1) / NB);
+    g.splits = splits;
+    g.part_ld = (g.N + 3) / 4 * 4;
     k_gemm<T, BM, BN, NWM, NWN, kAT, kBT, KIND>
-        <<<dim3((unsigned)(g.tiles_m * g.tiles_n), 1, (unsigned)batch), dim3(NWM * NWN * 64), 0, s>>>(g);
-    return hipGetLastError();
+        <<<dim3((unsigned)(g.tiles_m * g.tiles_n), 1, (unsigned)(g.batch * splits)), dim3(NWM * NWN * 64), 0, s>>>(g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    return join(g.part, g.part_ld, splits, g.M, g.N, g.c[0], g.c[1], g.batch, g.ldc, sizeof(T) == 4 || g.f32_out, s);
 }
 
-template <typename T, bool kAT, bool kBT, Kind KIND> hipError_t pick(const GemmArgs &g, int batch, hipStream_t s) {
-    if constexpr (sizeof(T) == 2) return run<T, 256, 256, 2, 4, kAT, kBT, KIND>(g, batch, s);
-    else return run<T, 128, 128, 2, 2, kAT, kBT, KIND>(g, batch, s);
+// Tile and split of a product.  Estimated time: rounds of resident workgroups
+// times a tile's steps, in units of the small tile's step.
+struct Choice {
+    bool big;
+    int splits;
+};
+template <typename T> Choice choose(const GemmArgs &g, bool gates) {
+    constexpr int kBig = sizeof(T) == 2 ? 256 : 128, kSmall = kBig / 2, BK = kRowBytes / sizeof(T);
+    const int64_t n = gates ? 2 * g.ldc : g.N, steps = (g.K + BK - 1) / BK * g.nseg;
+    Choice best{true, 1};
+    double tbest = -1.0;
+    for (const bool big : {true, false}) {
+        const int64_t b = big ? kBig : kSmall, tiles = (g.M + b - 1) / b * ((n + b - 1) / b) * g.batch;
+        const int64_t slots = 256 * (big ? (sizeof(T) == 2 ? 1 : 2) : (sizeof(T) == 2 ? 2 : 4));
+        const double step = big ? 3.0 : 1.0, base = 6.0;
+        for (int splits = 1; splits <= (gates ? 1 : 16); ++splits) {
+            if (splits > 1 && (steps / splits < 4 || (size_t)splits * g.batch * g.M * ((g.N + 3) / 4 * 4) * 4 > kPartBytes)) break;
+            const double rounds = (double)((tiles * splits + slots - 1) / slots);
+            const double t = rounds * ((double)((steps + splits - 1) / splits) * step + base) + (splits > 1 ? 6.0 : 0.0);
+            if (tbest < 0.0 || t < tbest) { tbest = t; best = Choice{big, splits}; }
+        }
+    }
+    return best;
 }
 
-template <typename T> hipError_t dispatch(const GemmArgs &g, bool at, bool bt, Kind kind, int batch, hipStream_t s) {
-    if (kind == kGate) return pick<T, false, false, kGate>(g, batch, s);
-    if (kind == kGateBwd) return pick<T, false, false, kGateBwd>(g, batch, s);
-    if (kind == kStoreF32) return pick<T, false, true, kStoreF32>(g, batch, s);
-    if (at) return pick<T, true, true, kStore>(g, batch, s);
-    return bt ? pick<T, false, true, kStore>(g, batch, s) : pick<T, false, false, kStore>(g, batch, s);
+template <typename T, bool kAT, bool kBT, Kind KIND> hipError_t pick(const GemmArgs &g, hipStream_t s) {
+    const Choice c = choose<T>(g, KIND != kStore);
+    if constexpr (sizeof(T) == 2)
+        return c.big ? run<T, 256, 256, 2, 4, kAT, kBT, KIND>(g, c.splits, s) : run<T, 128, 128, 2, 2, kAT, kBT, KIND>(g, c.splits, s);
+    else if constexpr (KIND != kStore)
+        return c.big ? run<T, 128, 128, 2, 2, kAT, kBT, KIND>(g, c.splits, s) : run<T, 64, 64, 4, 1, kAT, kBT, KIND>(g, c.splits, s);
+    else
+        return c.big ? run<T, 128, 128, 2, 2, kAT, kBT, KIND>(g, c.splits, s) : run<T, 64, 64, 2, 2, kAT, kBT, KIND>(g, c.splits, s);
+}
+
+template <typename T> hipError_t dispatch(const GemmArgs &g, bool at, bool bt, Kind kind, hipStream_t s) {
+    if (kind == kGate) return pick<T, false, false, kGate>(g, s);
+    if (kind == kGateBwd) return pick<T, false, false, kGateBwd>(g, s);
+    if (at) return pick<T, true, true, kStore>(g, s);
+    return bt ? pick<T, false, true, kStore>(g, s) : pick<T, false, false, kStore>(g, s);
 }
 
 }  // namespace
 
-hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, int batch, hipStream_t s) {
-    return f32 ? dispatch<float>(g, at, bt, kind, batch, s) : dispatch<bf16>(g, at, bt, kind, batch, s);
+hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, hipStream_t s) {
+    return f32 ? dispatch<float>(g, at, bt, kind, s) : dispatch<bf16>(g, at, bt, kind, s);
 }
 hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s) {
     if (f32) return gates ? few_rows<float, true>(a, s) : few_rows<float, false>(a, s);

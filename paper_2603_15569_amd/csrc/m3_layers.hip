@@ -18,6 +18,8 @@ namespace {
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+// Workgroups of one launch (a grid's threads are counted in 32 bits)
+constexpr int64_t kMostGroups = INT64_C(1) << 22;
 m3_status launched(hipError_t e) {
     if (e == hipSuccess) return M3_OK;
     note_hip_error(e);
@@ -55,10 +57,10 @@ m3_status check_glr(const m3_glr_dims *d, bool step) {
     if (d->batch > INT_MAX || d->width > INT_MAX || d->batch * d->width > kMost / L) return M3_ERR_SHAPE;
     for (int64_t s : strides)
         if (s < 0 || s > kMost / std::max(L, d->batch)) return M3_ERR_SHAPE;
-    if (step) return d->batch * d->width / 256 < INT_MAX ? M3_OK : M3_ERR_SHAPE;
-    // one workgroup a tile, counted in 31 bits (groups of 64 channels: the most)
+    if (step) return d->batch * d->width / 256 < kMostGroups ? M3_OK : M3_ERR_SHAPE;
+    // one workgroup a tile (groups of 64 channels: the most)
     const int64_t tiles = (d->seqlen + glr::kChunk - 1) / glr::kChunk, groups = (d->width + 63) / 64;
-    if (d->batch * groups > INT_MAX / std::max<int64_t>(tiles, 1)) return M3_ERR_SHAPE;
+    if (d->batch * groups > kMostGroups / std::max<int64_t>(tiles, 1)) return M3_ERR_SHAPE;
     return M3_OK;
 }
 
@@ -194,15 +196,15 @@ namespace {
 m3_status check_ffn(const m3_ffn_dims *d, bool bwd) {
     if (!d) return M3_ERR_NULL;
     if (d->io != M3_F32 && d->io != M3_BF16) return M3_ERR_DTYPE;
-    constexpr int64_t kMost = INT64_C(1) << 20;   // (a tile's rows within 31-bit offsets)
+    constexpr int64_t kMost = INT64_C(1) << 16;   // (a tile's rows stay within 31-bit offsets)
     if (d->tokens < 0 || d->dmodel < 1 || d->dff < 1 || d->dmodel > kMost || d->dff > kMost) return M3_ERR_SHAPE;
     if (d->tokens > (INT64_C(1) << 40) / std::max(d->dmodel, d->dff)) return M3_ERR_SHAPE;
     if (d->act != M3_ACT_SILU && d->act != M3_ACT_GELU) return M3_ERR_SHAPE;
-    if (d->x_stride < d->dmodel || d->x_stride > kMost) return M3_ERR_SHAPE;
-    if (bwd && (d->dy_stride < d->dmodel || d->dy_stride > kMost)) return M3_ERR_SHAPE;
-    // one workgroup a tile of 64 (gates) or 128 columns and 128 rows, counted in 31 bits
-    const int64_t rows = std::max(d->tokens, std::max(d->dmodel, d->dff)) / 128 + 1;
-    if (rows > INT_MAX / (std::max(d->dmodel, d->dff) / 64 + 1)) return M3_ERR_SHAPE;
+    if (d->x_stride < d->dmodel || d->x_stride > 16 * kMost) return M3_ERR_SHAPE;
+    if (bwd && (d->dy_stride < d->dmodel || d->dy_stride > 16 * kMost)) return M3_ERR_SHAPE;
+    // the smallest tiles, 64 rows by 32 columns of a gate, in one launch
+    const int64_t rows = std::max(d->tokens, std::max(d->dmodel, d->dff)) / 64 + 1;
+    if (rows > kMostGroups / (std::max(d->dmodel, d->dff) / 32 + 1)) return M3_ERR_SHAPE;
     return M3_OK;
 }
 
@@ -210,7 +212,7 @@ m3_status check_ffn(const m3_ffn_dims *d, bool bwd) {
 struct FfnLayout {
     int64_t Dp, Fp;
     bool pad_d, pad_f;             // weights with rows of dmodel, of dff, are copied
-    size_t x, dy, wg, wu, wd, h, dg, du, dh, total;
+    size_t x, dy, wg, wu, wd, h, dg, du, dh, part, total;
 };
 FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
     const int64_t e = d->io == M3_F32 ? 4 : 2, el = 16 / e;
@@ -234,7 +236,8 @@ FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
     w.dg = bwd ? take(d->tokens, w.Fp, e) : 0;
     w.du = bwd ? take(d->tokens, w.Fp, e) : 0;
     w.dh = bwd ? take(d->tokens, w.Fp, 4) : 0;
-    w.total = at + 256;
+    w.part = take(1, (int64_t)ffn::kPartBytes, 1);
+    w.total = at;
     return w;
 }
 
@@ -258,14 +261,15 @@ struct Ffn {
         if (e == hipSuccess && rows > 0) e = ffn::launch_pad(p, ld, ws + at, padded, rows, cols, f32, stream);
         return Rows{ws + at, padded};
     }
-    void gemm(const ffn::GemmArgs &g, bool at, bool bt, ffn::Kind kind, int batch) {
-        if (e == hipSuccess && g.M > 0 && g.N > 0) e = ffn::launch_gemm(g, f32, at, bt, kind, batch, stream);
+    void gemm(const ffn::GemmArgs &g, bool at, bool bt, ffn::Kind kind) {
+        if (e == hipSuccess && g.M > 0 && g.N > 0) e = ffn::launch_gemm(g, f32, at, bt, kind, stream);
     }
     ffn::GemmArgs args(int64_t M, int64_t N, int64_t K, Rows a, Rows b, void *c, int64_t ldc) const {
         ffn::GemmArgs g = {};
         g.a[0] = g.a[1] = a.p; g.b[0] = g.b[1] = b.p;
         g.lda = a.ld; g.ldb = b.ld;
-        g.M = M; g.N = N; g.K = K; g.nseg = 1;
+        g.M = M; g.N = N; g.K = K; g.nseg = g.batch = 1;
+        g.part = reinterpret_cast<float *>(ws + w.part);
         g.c[0] = g.c[1] = c; g.ldc = ldc;
         g.gelu = d->act == M3_ACT_GELU;
         return g;
@@ -304,16 +308,16 @@ extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd), h{f.ws + w.h, w.Fp};
     if (T <= ffn::kFewRows && f.e == hipSuccess) {
         // (K in whole pieces: the copies are padded with zeros, and so is h)
-        ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU};
+        ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU, nullptr, 1};
         f.e = ffn::launch_few(a, f.f32, true, f.stream);
-        a = ffn::FewArgs{h.p, {rd.p, rd.p}, h.ld, rd.ld, T, D, w.Fp, D, y, D, 0};
+        a = ffn::FewArgs{h.p, {rd.p, rd.p}, h.ld, rd.ld, T, D, w.Fp, D, y, D, 0, reinterpret_cast<float *>(f.ws + w.part), 1};
         if (f.e == hipSuccess) f.e = ffn::launch_few(a, f.f32, false, f.stream);
         return launched(f.e);
     }
     ffn::GemmArgs g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
     g.b[1] = ru.p;
-    f.gemm(g, false, false, ffn::kGate, 1);
-    f.gemm(f.args(T, D, F, h, rd, y, D), false, false, ffn::kStore, 1);
+    f.gemm(g, false, false, ffn::kGate);
+    f.gemm(f.args(T, D, F, h, rd, y, D), false, false, ffn::kStore);
     return launched(f.e);
 }
 
@@ -333,22 +337,24 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd);
     const Rows h{f.ws + w.h, w.Fp}, dg{f.ws + w.dg, w.Fp}, du{f.ws + w.du, w.Fp};
     // dh = dy Wd (with the padding's columns, zero, too)
-    f.gemm(f.args(T, w.Fp, D, ry, rd, f.ws + w.dh, w.Fp), false, true, ffn::kStoreF32, 1);
+    ffn::GemmArgs g = f.args(T, w.Fp, D, ry, rd, f.ws + w.dh, w.Fp);
+    g.f32_out = 1;
+    f.gemm(g, false, true, ffn::kStore);
     // g and u again; h, dg, du
-    ffn::GemmArgs g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
+    g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
     g.b[1] = ru.p;
     g.dg = f.ws + w.dg; g.du = f.ws + w.du;
     g.dh = reinterpret_cast<const float *>(f.ws + w.dh);
-    f.gemm(g, false, false, ffn::kGateBwd, 1);
+    f.gemm(g, false, false, ffn::kGateBwd);
     // dx = dg Wg + du Wu
     g = f.args(T, D, F, dg, rg, dx, D);
     g.a[1] = du.p; g.b[1] = ru.p; g.nseg = 2;
-    f.gemm(g, false, true, ffn::kStore, 1);
+    f.gemm(g, false, true, ffn::kStore);
     // dWg = dg^T x, dWu = du^T x
     g = f.args(F, D, T, dg, rx, dWg, D);
-    g.a[1] = du.p; g.c[1] = dWu;
-    f.gemm(g, true, true, ffn::kStore, 2);
-    f.gemm(f.args(D, F, T, ry, h, dWd, F), true, true, ffn::kStore, 1);
+    g.a[1] = du.p; g.c[1] = dWu; g.batch = 2;
+    f.gemm(g, true, true, ffn::kStore);
+    f.gemm(f.args(D, F, T, ry, h, dWd, F), true, true, ffn::kStore);
     return launched(f.e);
 }
 
@@ -369,7 +375,7 @@ extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_tens
     for (int64_t k = 0; k < count; ++k) {   // all of them before the first launch
         const m3_adamw_tensor &t = tensors[k];
         if (t.n < 0 || !std::isfinite(t.decay)) return M3_ERR_SHAPE;
-        if (t.n / adamw::kChunkElems >= INT_MAX / (2 * adamw::kTensors)) return M3_ERR_SHAPE;
+        if (t.n / adamw::kChunkElems >= kMostGroups) return M3_ERR_SHAPE;
         if (t.n == 0) continue;
         if (!t.p || !t.g || !t.m || !t.v || (eight && !t.scales)) return M3_ERR_NULL;
         if (!aligned(t.p, 4) || !aligned(t.g, gf32 ? 4 : 2) || !aligned(t.low, 2) || (eight && !aligned(t.scales, 4)) ||
@@ -388,9 +394,10 @@ extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_tens
         for (; k < count && a.count < adamw::kTensors; ++k) {
             const m3_adamw_tensor &t = tensors[k];
             if (t.n == 0) continue;
+            const int64_t chunks = (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
+            if (a.count > 0 && a.start[a.count] + chunks > kMostGroups) break;
             a.t[a.count] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, t.n, (float)(1.0 - c->lr * t.decay),
                                          (uint32_t)(c->seed + (uint64_t)k)};
-            const int64_t chunks = (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
             a.start[a.count + 1] = a.start[a.count] + (int32_t)chunks;
             ++a.count;
         }
