@@ -86,28 +86,34 @@ template <typename T> __device__ __forceinline__ uint32_t span(int64_t rows, int
 }
 
 // Operand fragments of 16 rows by 64 bytes of k (kk = 0, 1): lane (q, l16) holds
-// 16 bytes of k of row l16.
-template <typename T, bool kPair>
-__device__ __forceinline__ f32x4 frag(const char *tile, int row, int kk, int q) {
-    return *reinterpret_cast<const f32x4 *>(tile + row * kRowBytes + ((kk * 4 + q) ^ spread<kPair>(row)) * 16);
-}
-template <typename T, int ROWS>
-__device__ __forceinline__ f32x4 frag_turned(const char *tile, int c0, int kk, int q, int l16) {
-    constexpr int W = ROWS * (int)sizeof(T);
-    if constexpr (sizeof(T) == 2) {
-        const int k = kk * 32 + 8 * q + l16 / 4;
-        const char *p0 = tile + k * W + ((c0 / 16) ^ turn<T>(k)) * 32 + (l16 % 4) * 8;
-        const char *p1 = tile + (k + 4) * W + ((c0 / 16) ^ turn<T>(k + 4)) * 32 + (l16 % 4) * 8;
-        const bf16x4 lo = scan::lds_tr4(reinterpret_cast<const bf16 *>(p0));
-        const bf16x4 hi = scan::lds_tr4(reinterpret_cast<const bf16 *>(p1));
-        return __builtin_bit_cast(f32x4, scan::cat4(lo, hi));
+// 16 bytes of k of row l16.  `at` is where the lane's piece of the fragment is
+// at kk = 0 in a [row][k] tile, and in a turned one at kk = 0 and for its first
+// four (bf16) or one (fp32) of k.
+template <typename T, int ROWS, bool kTurned, bool kPair>
+__device__ __forceinline__ uint32_t frag_at(int row0, int i, int q, int l16) {
+    if constexpr (!kTurned) {
+        // (pairs of tiles: the tile's row r is column 8 (r / 4) + r % 4, + 4 in odd tiles, of 32)
+        const int row = row0 + (kPair ? i / 2 * 32 + l16 / 4 * 8 + l16 % 4 + i % 2 * 4 : 16 * i + l16);
+        return (uint32_t)(row * kRowBytes + (q ^ spread<kPair>(row)) * 16);
     } else {
+        constexpr int W = ROWS * (int)sizeof(T);
+        const int k = sizeof(T) == 2 ? 8 * q + l16 / 4 : 4 * q, blk = (row0 / 16 + i) ^ turn<T>(k);
+        return (uint32_t)(k * W + blk * (16 * (int)sizeof(T)) + (sizeof(T) == 2 ? l16 % 4 * 8 : l16 * 4));
+    }
+}
+template <typename T, int ROWS, bool kTurned>
+__device__ __forceinline__ f32x4 frag(const char *tile, uint32_t at, int kk) {
+    constexpr int W = ROWS * (int)sizeof(T);
+    if constexpr (!kTurned) {
+        return *reinterpret_cast<const f32x4 *>(tile + (at ^ (uint32_t)(kk * 64)));
+    } else if constexpr (sizeof(T) == 2) {   // (rows k and k + 4, and k + 32, turn alike)
+        const bf16x4 lo = scan::lds_tr4(reinterpret_cast<const bf16 *>(tile + at + kk * 32 * W));
+        const bf16x4 hi = scan::lds_tr4(reinterpret_cast<const bf16 *>(tile + at + (kk * 32 + 4) * W));
+        return __builtin_bit_cast(f32x4, scan::cat4(lo, hi));
+    } else {                                 // (rows k .. k + 3, and k + 16, turn alike)
         f32x4 v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = kk * 16 + 4 * q + j;
-            v[j] = *reinterpret_cast<const float *>(tile + k * W + ((c0 / 16) ^ turn<T>(k)) * 64 + l16 * 4);
-        }
+        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float *>(tile + at + (kk * 16 + j) * W);
         return v;
     }
 }
@@ -222,32 +228,55 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    if (it0 < it1) load(it0);
-    for (int it = it0; it < it1; ++it) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's pieces of the stage have landed (vmcnt 0)
-        __syncthreads();                      // everyone's have, and the other stage has been read
-        if (it + 1 < it1) load(it + 1);
-        const char *sa = lds[it & 1], *sb = sa + BM * kRowBytes;
+    // Where the lane's fragments are in a stage
+    uint32_t fa_at[MT], fb_at[NT];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            f32x4 fb[NT];
+    for (int i = 0; i < MT; ++i) fa_at[i] = frag_at<T, BM, kAT, false>(wm * WM, i, q, l16);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if constexpr (kBT) {
-                    fb[j] = frag_turned<T, BN>(sb, wn * WN + 16 * j, kk, q, l16);
-                } else {
-                    // the tile's row r is column 8 (r / 4) + r % 4 (+ 4 in odd tiles) of 32
-                    fb[j] = frag<T, kPair>(sb, wn * WN + j / 2 * 32 + l16 / 4 * 8 + l16 % 4 + j % 2 * 4, kk, q);
-                }
-            }
+    for (int j = 0; j < NT; ++j) fb_at[j] = BM * kRowBytes + frag_at<T, BN, kBT, kPair>(wn * WN, j, q, l16);
+    auto read = [&](int it, int kk, f32x4 (&fa)[MT], f32x4 (&fb)[NT]) {
+        const char *stage = lds[it & 1];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const f32x4 fa = kAT ? frag_turned<T, BM>(sa, wm * WM + 16 * i, kk, q, l16)
-                                     : frag<T, false>(sa, wm * WM + 16 * i + l16, kk, q);
+        for (int j = 0; j < NT; ++j) fb[j] = frag<T, BN, kBT>(stage, fb_at[j], kk);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa, acc[i][j]);
-            }
+        for (int i = 0; i < MT; ++i) fa[i] = frag<T, BM, kAT>(stage, fa_at[i], kk);
+    };
+    auto multiply = [&](const f32x4 (&fa)[MT], const f32x4 (&fb)[NT]) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
+    };
+    // One half of a stage is multiplied while the next half is read: the
+    // matrix units never wait for LDS, and a stage's loads have a whole step
+    // to land.  The schedule spreads the reads over the products.
+    constexpr int kReads = MT * (kAT ? (sizeof(T) == 2 ? 2 : 4) : 1) + NT * (kBT ? (sizeof(T) == 2 ? 2 : 4) : 1);
+    constexpr int kMmas = MT * NT * (sizeof(T) == 2 ? 1 : 4), kEach = kMmas / kReads > 0 ? kMmas / kReads : 1;
+    auto interleave = [&]() {
+#pragma unroll
+        for (int k = 0; k < kReads; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);  // products
         }
+    };
+    f32x4 a0[MT], b0[NT], a1[MT], b1[NT];
+    if (it0 < it1) {
+        load(it0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt 0: this wave's pieces have landed)
+        __syncthreads();
+        if (it0 + 1 < it1) load(it0 + 1);
+        read(it0, 0, a0, b0);
+    }
+    for (int it = it0; it < it1; ++it) {
+        read(it, 1, a1, b1);
+        multiply(a0, b0);
+        interleave();
+        __builtin_amdgcn_s_waitcnt(0x0070);   // the next stage has landed, this one has been read
+        __syncthreads();                      // by every wave
+        if (it + 2 < it1) load(it + 2);
+        read(it + 1, 0, a0, b0);              // (past the last stage: never used)
+        multiply(a1, b1);
+        interleave();
     }
 
     // A lane holds row m = l16 of each 16-row tile, and four columns of each of
