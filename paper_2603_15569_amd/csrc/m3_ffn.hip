@@ -38,12 +38,24 @@ template <typename T> __device__ __forceinline__ int turn(int k) {
     return sizeof(T) == 2 ? (k & 3) | (k >> 1 & 4) : k >> 2 & 3;
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
+// A buffer resource's words, in scalar registers
+typedef int Words __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Words make_words(const void *base, uint32_t bytes) {
+    const uint64_t p = (uint64_t)(uintptr_t)base;
+    return Words{(int)(uint32_t)p, (int)(uint32_t)(p >> 32), (int)bytes, 0x00020000};
+}
 
 // One 16-byte piece a lane from `off` bytes into a buffer to LDS: lane l's goes
-// to `to` + 16 l.
-__device__ __forceinline__ void load_lds(Rsrc r, uint32_t off, char *to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)to, 16, (int)off, 0, 0, 0);
+// to `to` + 16 l.  In assembly, so that the compiler, which cannot tell the two
+// stages apart, does not wait for these loads before it reads the other stage:
+// the kernel waits for them itself (vmcnt 0 and a barrier) before it reads
+// theirs.  (The loads write no register.)
+__device__ __forceinline__ void load_lds(Words r, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const char *p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
 }
 
 // An operand tile's loads: ROWS rows of the operand by 128 bytes of k.
@@ -163,8 +175,11 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     constexpr int GM = 8;
     const int grp = t / (GM * g.tiles_n), in = t % (GM * g.tiles_n);
     const int gm = min(GM, g.tiles_m - grp * GM);
-    const int64_t m0 = (int64_t)(grp * GM + in % gm) * BM, n0 = (int64_t)(in / gm) * NB;
-    const int z = (int)blockIdx.z / g.splits, split = (int)blockIdx.z % g.splits;
+    // (divisions leave their results in vector registers: back to scalar ones,
+    // where addresses and resources are formed)
+    auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int64_t m0 = (int64_t)scalar(grp * GM + in % gm) * BM, n0 = (int64_t)scalar(in / gm) * NB;
+    const int z = scalar((int)blockIdx.z / g.splits), split = scalar((int)blockIdx.z % g.splits);
 
     Tile<T, BM, NW, kAT, false> ta;
     Tile<T, BN, NW, kBT, kPair> tb;
@@ -180,45 +195,54 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
         tb.init(g.ldb, wave, lane);
     }
 
-    const int nk = (int)((g.K + BK - 1) / BK), steps = nk * g.nseg;
-    const int it0 = (int)((int64_t)steps * split / g.splits), it1 = (int)((int64_t)steps * (split + 1) / g.splits);
-    auto load = [&](int it) {
-        const int seg = it >= nk ? 1 : 0;
-        const int64_t k0 = (int64_t)(it - seg * nk) * BK;
-        const bool tail = k0 + BK > g.K;
-        char *stage = lds[it & 1];
-        const T *pa = static_cast<const T *>(g.a[kGates ? 0 : z + seg]);
-        const Rsrc ra = kAT ? make_rsrc(pa + k0 * g.lda + m0, span<T>(g.K - k0, g.lda, g.M - m0, BK))
-                            : make_rsrc(pa + m0 * g.lda + k0, span<T>(g.M - m0, g.lda, g.K - k0, BM));
+    const int K = (int)g.K, nk = (K + BK - 1) / BK, steps = nk * g.nseg;
+    const int it0 = scalar((int)((int64_t)steps * split / g.splits)), it1 = scalar((int)((int64_t)steps * (split + 1) / g.splits));
+    // The tile's operands at k = 0 of the first and of the second product summed
+    auto at0 = [](const void *p, bool turned, int64_t ld, int64_t r0) { return static_cast<const T *>(p) + (turned ? r0 : r0 * ld); };
+    const T *pa0 = at0(g.a[kGates ? 0 : z], kAT, g.lda, m0), *pa1 = kGates ? pa0 : at0(g.a[(z + 1) & 1], kAT, g.lda, m0);
+    const T *pb0 = at0(g.b[kGates ? 0 : z], kBT, g.ldb, n0), *pb1 = at0(g.b[kGates ? 1 : (z + 1) & 1], kBT, g.ldb, n0);
+    if constexpr (kGates && NW == 8) {   // (a wave's rows are all of Wg, or all of Wu)
+        if (wave >= 4) pb0 = pb1;
+    }
+    // A stage's resource: zero past the rows, past k, and after the last step.
+    // No branches: the scalar work and the loads go in between the products.
+    const uint32_t lda = (uint32_t)(g.lda * sizeof(T)), ldb = (uint32_t)(g.ldb * sizeof(T));
+    const uint32_t sa0 = kAT ? span<T>(1, 0, g.M - m0, 1) : span<T>(g.M - m0, g.lda, g.K, BM);
+    const uint32_t sb0 = kBT ? span<T>(1, 0, g.N - n0, 1) : span<T>(g.N - n0, g.ldb, g.K, NB);
+    auto stage_rsrc = [&](const T *p, bool turned, uint32_t ld, uint32_t span0, int k0, bool in) {
+        const int rows = min(K - k0, BK);
+        const uint32_t n = turned ? (uint32_t)(rows - 1) * ld + span0 : span0 - (uint32_t)k0 * (uint32_t)sizeof(T);
+        const char *base = reinterpret_cast<const char *>(p) + (turned ? (int64_t)k0 * ld : (int64_t)k0 * (int64_t)sizeof(T));
+        return make_words(base, in ? n : 0u);
+    };
+    struct Stage {
+        Words ra, rb, ru;
+        int left;       // of k
+        uint32_t to;
+    };
+    auto stage = [&](int it) {
+        const bool in = it < it1, second = it >= nk;
+        const int k0 = (second && g.nseg > 1 ? it - nk : it) * BK;
+        Stage s;
+        s.ra = stage_rsrc(second ? pa1 : pa0, kAT, lda, sa0, k0, in);
+        s.rb = stage_rsrc(!kGates && second ? pb1 : pb0, kBT, ldb, sb0, k0, in);
+        s.ru = kGates && NW != 8 ? stage_rsrc(pb1, kBT, ldb, sb0, k0, in) : s.rb;
+        s.left = K - k0;
+        s.to = lds_address(lds[0]) + (uint32_t)(it & 1) * (uint32_t)sizeof lds[0];
+        return s;
+    };
+    auto load = [&](const Stage &s) {
 #pragma unroll
         for (int j = 0; j < ta.NI; ++j) {
             uint32_t off = ta.off[j];
-            if constexpr (!kAT)
-                if (tail && k0 + ta.k_of(j, wave, lane) >= g.K) off = kOut;
-            load_lds(ra, off, stage + (j * NW + wave) * 1024);
+            if constexpr (!kAT) off = ta.k_of(j, wave, lane) >= s.left ? kOut : off;
+            load_lds(s.ra, off, s.to + (j * NW + wave) * 1024);
         }
-        stage += BM * kRowBytes;
-        if constexpr (kGates) {
 #pragma unroll
-            for (int j = 0; j < tb.NI; ++j) {
-                const int which = (j * NW + wave) * 8 % 64 / 32;
-                const T *pb = static_cast<const T *>(which ? g.b[1] : g.b[0]);
-                const Rsrc rb = make_rsrc(pb + n0 * g.ldb + k0, span<T>(g.N - n0, g.ldb, g.K - k0, NB));
-                uint32_t off = tb.off[j];
-                if (tail && k0 + tb.k_of(j, wave, lane) >= g.K) off = kOut;
-                load_lds(rb, off, stage + (j * NW + wave) * 1024);
-            }
-        } else {
-            const T *pb = static_cast<const T *>(g.b[z + seg]);
-            const Rsrc rb = kBT ? make_rsrc(pb + k0 * g.ldb + n0, span<T>(g.K - k0, g.ldb, g.N - n0, BK))
-                                : make_rsrc(pb + n0 * g.ldb + k0, span<T>(g.N - n0, g.ldb, g.K - k0, BN));
-#pragma unroll
-            for (int j = 0; j < tb.NI; ++j) {
-                uint32_t off = tb.off[j];
-                if constexpr (!kBT)
-                    if (tail && k0 + tb.k_of(j, wave, lane) >= g.K) off = kOut;
-                load_lds(rb, off, stage + (j * NW + wave) * 1024);
-            }
+        for (int j = 0; j < tb.NI; ++j) {
+            uint32_t off = tb.off[j];
+            if constexpr (!kBT) off = tb.k_of(j, wave, lane) >= s.left ? kOut : off;
+            load_lds(kGates && NW != 8 && j % 2 ? s.ru : s.rb, off, s.to + BM * kRowBytes + (j * NW + wave) * 1024);
         }
     };
 
@@ -261,23 +285,26 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     };
     f32x4 a0[MT], b0[NT], a1[MT], b1[NT];
     if (it0 < it1) {
-        load(it0);
+        load(stage(it0));
         __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt 0: this wave's pieces have landed)
         __syncthreads();
-        if (it0 + 1 < it1) load(it0 + 1);
+        load(stage(it0 + 1));
         read(it0, 0, a0, b0);
     }
     for (int it = it0; it < it1; ++it) {
         read(it, 1, a1, b1);
+        const Stage next = stage(it + 2);
         multiply(a0, b0);
         interleave();
         __builtin_amdgcn_s_waitcnt(0x0070);   // the next stage has landed, this one has been read
         __syncthreads();                      // by every wave
-        if (it + 2 < it1) load(it + 2);
-        read(it + 1, 0, a0, b0);              // (past the last stage: never used)
+        load(next);
+        __builtin_amdgcn_sched_barrier(0);    // (as early as can be)
+        read(it + 1, 0, a0, b0);              // (past the last stage: zeros, never used)
         multiply(a1, b1);
         interleave();
     }
+    __builtin_amdgcn_s_waitcnt(0x0F70);       // (nothing may land in LDS after the workgroup's end)
 
     // A lane holds row m = l16 of each 16-row tile, and four columns of each of
     // the NT column tiles: 4 q .. 4 q + 3, or (pairs of tiles) 8 q .. 8 q + 7.
