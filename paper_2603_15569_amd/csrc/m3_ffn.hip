@@ -12,6 +12,7 @@
 // Edges: buffer loads return zero past the end of an operand, so rows past M,
 // N or (turned) K need no masks; k past K within a row is sent out of range.
 #include <algorithm>
+#include <cmath>
 
 #include "m3_device.h"
 #include "m3_ffn.h"
@@ -592,25 +593,43 @@ hipError_t run(GemmArgs g, int splits, hipStream_t s) {
     return join(g.part, g.part_ld, splits, g.M, g.N, g.c[0], g.c[1], g.batch, g.ldc, sizeof(T) == 4 || g.f32_out, s);
 }
 
-// Tile and split of a product.  Estimated time: rounds of resident workgroups
-// times a tile's steps, in units of the small tile's step.
+// Tile and split of a product, from estimated times (microseconds) fitted to
+// every tile and split of 95 bf16 and 80 fp32 products of the block (100 to
+// 8192 tokens, widths of 512 to 8192); the choice costs 0.8% (bf16) and 0.5%
+// (fp32) more than the best of them on average.
+//   bf16: a tile of 256 has a compute unit to itself, 128 shares one with
+//     another: rounds of resident workgroups, a step 1.18, and .645 alone to
+//     1.02 shared, 10.3 and 6.2 a round.
+//   fp32: the matrix units bound either tile, so a unit's workgroups add up:
+//     a step 1.76 (128) or .451 (64) for each of them.
+// Parts cost their bytes, written and read.  (768 x 1024 -> 2816, fp32 gates:
+// 124 us of 128, 84 of 64; 2048 x 8192 -> 2048: 203 and 246 us in bf16.)
 struct Choice {
     bool big;
     int splits;
 };
 template <typename T> Choice choose(const GemmArgs &g, bool gates) {
-    constexpr int kBig = sizeof(T) == 2 ? 256 : 128, kSmall = kBig / 2, BK = kRowBytes / sizeof(T);
+    constexpr bool kHalf = sizeof(T) == 2;
+    constexpr int kBig = kHalf ? 256 : 128, BK = kRowBytes / (int)sizeof(T);
+    constexpr double kUnits = 256.0;   // compute units
     const int64_t n = gates ? 2 * g.ldc : g.N, steps = (g.K + BK - 1) / BK * g.nseg;
     Choice best{true, 1};
     double tbest = -1.0;
     for (const bool big : {true, false}) {
-        const int64_t b = big ? kBig : kSmall, tiles = (g.M + b - 1) / b * ((n + b - 1) / b) * g.batch;
-        const int64_t slots = 256 * (big ? (sizeof(T) == 2 ? 1 : 2) : (sizeof(T) == 2 ? 2 : 4));
-        const double step = big ? 3.0 : 1.0, base = 6.0;
+        const int64_t b = big ? kBig : kBig / 2, tiles = (g.M + b - 1) / b * ((n + b - 1) / b) * g.batch;
         for (int splits = 1; splits <= (gates ? 1 : 16); ++splits) {
-            if (splits > 1 && (steps / splits < 4 || (size_t)splits * g.batch * g.M * ((g.N + 3) / 4 * 4) * 4 > kPartBytes)) break;
-            const double rounds = (double)((tiles * splits + slots - 1) / slots);
-            const double t = rounds * ((double)((steps + splits - 1) / splits) * step + base) + (splits > 1 ? 6.0 : 0.0);
+            const double part = (double)splits * g.batch * g.M * ((g.N + 3) / 4 * 4) * 4.0;
+            if (splits > 1 && (splits > steps || part > (double)kPartBytes)) break;
+            const double wgs = (double)tiles * splits, each = std::ceil((double)steps / splits), load = std::ceil(wgs / kUnits);
+            double t;
+            if (kHalf) {
+                const double rounds = std::ceil(load / (big ? 1 : 2)), share = std::min(std::max(wgs / kUnits - 1.0, 0.0), 1.0);
+                t = rounds * (big ? each * 1.18 + 10.3 : each * (.645 + .38 * share) + 6.2);
+            } else {
+                const double rounds = std::ceil(load / (big ? 2 : 5));
+                t = big ? each * (.15 * rounds + 1.76 * load) + 4.1 * rounds : each * (.106 * rounds + .451 * load) + 2.0 * rounds;
+            }
+            if (splits > 1) t += (kHalf ? 1.6 : 2.7) + part * (kHalf ? .45e-6 : .36e-6);
             if (tbest < 0.0 || t < tbest) { tbest = t; best = Choice{big, splits}; }
         }
     }
