@@ -520,7 +520,7 @@ void m3_set_wait_limit(uint32_t polls);
  * invalid dims).  It must be zero-filled before its first use and then be
  * used by m3_glr_* calls only, of any dims, one at a time.  Deterministic.
  * Alignment: the workspace 16 bytes, everything else its element's (else
- * M3_ERR_ALIGN); in bf16 two channels are moved at a time where the width, the
+ * M3_ERR_ALIGN); width and token strides at most 2^23.  In bf16 two channels are moved at a time where the width, the
  * strides and the token arrays' addresses are even in elements.  Outputs must
  * not overlap inputs.
  */

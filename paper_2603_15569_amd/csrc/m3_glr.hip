@@ -14,6 +14,8 @@
 // wait in registers meanwhile.  The backward runs the same way from the last
 // tile to the first on q_t = a_t (dh_t + q_{t+1}), with the states entering
 // the tiles as the forward saved them.
+#include <type_traits>
+
 #include "m3_device.h"
 #include "m3_glr.h"
 
@@ -33,12 +35,35 @@ __device__ __forceinline__ float get(uint16_t v, int) { return __uint_as_float((
 __device__ __forceinline__ float get(uint32_t v, int e) { return __uint_as_float(e ? v & 0xffff0000u : v << 16); }
 __device__ __forceinline__ float get(float v, int) { return v; }
 
-// Row access: a uniform pointer to the row and the lane's byte offset in it
-template <typename R> __device__ __forceinline__ R row_load(const void *row, uint32_t off) {
-    return *reinterpret_cast<const R *>(static_cast<const char *>(row) + off);
+// Up to `n` rows of an array from a uniform address on, as a buffer: a lane's
+// offset in the row in a vector register, the row's in a scalar one, so that
+// an access takes no address arithmetic.  Past the rows and past the width
+// (kOut) loads return zero and stores do nothing.  (A scalar offset past the
+// buffer's end would not be caught: rows from n on go to the first one with
+// kOut as the lane's offset.)
+constexpr uint32_t kOut = 0x80000000u;
+struct Rows {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t stride;
+    int n;
+};
+template <typename T> __device__ __forceinline__ Rows rows(const void *p, int64_t at, int64_t stride, int n, int64_t width) {
+    const uint32_t st = (uint32_t)(stride * sizeof(T));
+    const int bytes = n > 0 ? (int)((uint32_t)(n - 1) * st + (uint32_t)(width * sizeof(T))) : 0;
+    return Rows{__builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(p) + at), (short)0, bytes, 0x00020000), st, n};
 }
-template <typename R> __device__ __forceinline__ void row_store(void *row, uint32_t off, R v) {
-    *reinterpret_cast<R *>(static_cast<char *>(row) + off) = v;
+// (W: the buffer is known to hold the row)
+template <typename R, typename W> __device__ __forceinline__ R row_load(const Rows &w, int s, uint32_t off, W) {
+    const bool in = W::value || s < w.n;
+    const int lane = (int)(in ? off : kOut), row = in ? (int)(s * w.stride) : 0;
+    if constexpr (sizeof(R) == 2) return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b16(w.r, lane, row, 0));
+    else return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b32(w.r, lane, row, 0));
+}
+template <typename R, typename W> __device__ __forceinline__ void row_store(const Rows &w, int s, uint32_t off, R v, W) {
+    const bool in = W::value || s < w.n;
+    const int lane = (int)(in ? off : kOut), row = in ? (int)(s * w.stride) : 0;
+    if constexpr (sizeof(R) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w.r, lane, row, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w.r, lane, row, 0);
 }
 // Keeps the compiler from overlapping more tokens than registers are for.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
@@ -61,15 +86,15 @@ template <typename T, int V> __device__ __forceinline__ typename Raw<T, V>::type
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.f + exp2_fast(-kLog2e * v));
 }
-// a = e^l and w = sqrt(1 - a^2) of a log-decay l <= 0.  1 - a^2 = -2 a sinh(l):
-// near l = 0, where 1 - a^2 would keep few digits, by the series of sinh
-// (relative error below 2e-8 up to |l| = 0.5).
-__device__ __forceinline__ void decay(float l, float &a, float &w) {
-    a = exp2_fast(kLog2e * l);
+// 1 - a^2 of a decay a = 2^l, l <= 0: -2 a sinh(l ln 2) near l = 0, where the
+// plain form would keep few digits (by its series: relative error below 7e-8
+// up to |l ln 2| = 0.25).
+__device__ __forceinline__ float one_minus_square(float a, float l) {
+    constexpr float kLn2 = 0.693147180559945309417f, k3 = kLn2 * kLn2 * kLn2;
+    constexpr float c0 = -2.f * kLn2, c1 = -2.f * k3 / 6.f, c2 = -2.f * k3 * kLn2 * kLn2 / 120.f;
     const float q = l * l;
-    const float sh = fmaf(l * q, fmaf(q, fmaf(q, 1.f / 5040.f, 1.f / 120.f), 1.f / 6.f), l);
-    const float om = l > -0.5f ? -2.f * a * sh : fmaf(-a, a, 1.f);
-    w = __builtin_amdgcn_sqrtf(om);
+    const float near = a * l * fmaf(q, fmaf(q, c2, c1), c0);
+    return l > -0.25f / kLn2 ? near : fmaf(-a, a, 1.f);
 }
 // The state after a map (A, c) from the state h before it: one rounding order
 // everywhere, so that a fold of published maps and their owner's own state
@@ -89,35 +114,37 @@ __device__ __forceinline__ uint64_t get_word(const uint64_t *p) {
 __device__ __forceinline__ float word_value(uint64_t w) { return __uint_as_float((uint32_t)w); }
 
 struct Item {
-    int64_t tile;       // index of the tile in the order of its recurrence
-    int64_t b, grp;     // batch row, channel group
+    int tile;       // index of the tile in the order of its recurrence
+    int b, grp;     // batch row, channel group
     uint32_t tag;
 };
 
 // Work items in ticket order, tile-major: every tile that an item waits for
 // has an earlier ticket, so it is running or done.  The counter's upper half
-// is the count of calls on the workspace (the tag, never zero in use); whoever
-// takes the last ticket sets it up for the next call.
-__device__ __forceinline__ Item take_item(uint64_t *ctl, int64_t per_tile, int64_t tiles, int64_t G, uint64_t *s_ticket) {
-    if (tiles == 1) {
-        const int64_t k = blockIdx.x;
-        return Item{0, k / G, k % G, 0};
-    }
-    if (threadIdx.x == 0) {
-        const uint64_t w = __hip_atomic_fetch_add(ctl, (uint64_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if ((uint32_t)w == (uint32_t)(per_tile * tiles - 1)) {
-            const uint32_t epoch = (uint32_t)(w >> 32);
-            __hip_atomic_store(reinterpret_cast<uint32_t *>(ctl) + 2 + ((epoch + 1) & 1), 0u, __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(ctl, (uint64_t)(epoch + 1) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// is the count of calls on the workspace (plus one: the tag); whoever takes
+// the last ticket sets it up for the next call.
+__device__ __forceinline__ Item take_item(uint64_t *ctl, uint32_t B, uint32_t tiles, uint32_t G, uint64_t *s_ticket) {
+    // (divisions leave their results in vector registers: back to scalar ones)
+    auto scalar = [](uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); };
+    uint32_t k = blockIdx.x, tag = 0;
+    if (tiles > 1) {
+        if (threadIdx.x == 0) {
+            const uint64_t w = __hip_atomic_fetch_add(ctl, (uint64_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if ((uint32_t)w == B * G * tiles - 1) {
+                const uint32_t epoch = (uint32_t)(w >> 32);
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(ctl) + 2 + ((epoch + 1) & 1), 0u, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(ctl, (uint64_t)(epoch + 1) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            *s_ticket = w;
         }
-        *s_ticket = w;
+        __syncthreads();
+        const uint64_t w = *s_ticket;
+        k = (uint32_t)w;
+        tag = (uint32_t)(w >> 32) + 1u;
     }
-    __syncthreads();
-    const uint64_t w = *s_ticket;
-    const int64_t k = (int64_t)(uint32_t)w;
-    const int64_t in = k % per_tile;
-    return Item{k / per_tile, in / G, in % G, (uint32_t)(w >> 32) + 1u};
+    const uint32_t tile = k / (B * G), in = k - tile * (B * G), b = in / G;
+    return Item{scalar(tile), scalar(b), scalar(in - b * G), (uint32_t)scalar(tag)};
 }
 
 // Published words of a tile and channel: the state after the tile, and the
@@ -127,54 +154,75 @@ struct Words {
 };
 
 // The state that enters a tile (tile > 0, all threads of the workgroup).  Each
-// wave polls one of the NW tiles before this one; the nearest whose state is
-// known, with the maps of all after it, gives the state, folded in token
-// order.  `enter` is the state of the lane's channels, NaN when the wait gave up.
+// wave polls one of the NW tiles before this one; when that was not enough and
+// the sequence's start is in reach, kReach of them, back to `first`, the state
+// there (32 tiles of 512 channels: 13.9 us against 19.7 without; further into
+// a sequence the wider polling costs more than it saves, 261 us -> 284 at 512
+// tiles of 2048 channels).  The nearest tile whose state is known, with the
+// maps of all after it, gives the state, folded in token order.  `enter` is the state of the lane's channels,
+// NaN when the wait gave up.
+constexpr int kReach = 4;
+template <int V, int NW> struct Polled {
+    float v[kReach * NW][2][64 * V];   // the state after the tile, or its map
+    uint32_t kind[64];                 // 2: state, 1: map, 0: nothing yet
+};
 template <int V, int NW>
-__device__ __forceinline__ void look_back(const Words &wd, int64_t slot0, int64_t tile, int64_t D, int64_t d0, bool live,
+__device__ __forceinline__ void look_back(const Words &wd, int64_t slot0, int tile, int64_t D, int64_t d0, bool live,
                                           uint32_t tag, uint64_t *ctl, uint32_t spin_max, int wave, int lane,
-                                          float (*s_val)[3][64 * V], uint32_t *s_kind, float (&enter)[V]) {
+                                          const float (&first)[V], Polled<V, NW> &s, float (&enter)[V]) {
+    static_assert(kReach * NW <= 64, "a lane for each polled tile");
     for (uint32_t spin = 0;; ++spin) {
-        const int64_t j = tile - 1 - wave;
-        if (j >= 0) {
-            const int64_t at = slot0 + j * D + d0;
-            uint64_t wi[V], wa[V], wc[V];
-            bool inc = true, map = true;
+        const int reach = spin == 0 || tile > kReach * NW ? 1 : kReach;
+#pragma unroll 1
+        for (int r = 0; r < reach; ++r) {
+            const int p = r * NW + wave, j = tile - 1 - p;
+            uint32_t kind = 0;
+            float v[2][V];
+            if (j >= 0) {
+                const int64_t at = slot0 + j * D + d0;
+                uint64_t wi[V], wa[V], wc[V];
+                bool inc = true, map = true;
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                wi[e] = live ? get_word(wd.inc + at + e) : (uint64_t)tag << 32;
-                wa[e] = live ? get_word(wd.mapA + at + e) : (uint64_t)tag << 32;
-                wc[e] = live ? get_word(wd.mapC + at + e) : (uint64_t)tag << 32;
-            }
+                for (int e = 0; e < V; ++e) {
+                    wi[e] = live ? get_word(wd.inc + at + e) : (uint64_t)tag << 32;
+                    wa[e] = live ? get_word(wd.mapA + at + e) : (uint64_t)tag << 32;
+                    wc[e] = live ? get_word(wd.mapC + at + e) : (uint64_t)tag << 32;
+                }
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                inc = inc && (uint32_t)(wi[e] >> 32) == tag;
-                map = map && (uint32_t)(wa[e] >> 32) == tag && (uint32_t)(wc[e] >> 32) == tag;
-                s_val[wave][0][lane * V + e] = word_value(wi[e]);
-                s_val[wave][1][lane * V + e] = word_value(wa[e]);
-                s_val[wave][2][lane * V + e] = word_value(wc[e]);
+                for (int e = 0; e < V; ++e) {
+                    inc = inc && (uint32_t)(wi[e] >> 32) == tag;
+                    map = map && (uint32_t)(wa[e] >> 32) == tag && (uint32_t)(wc[e] >> 32) == tag;
+                }
+                kind = __all(inc) ? 2u : __all(map) ? 1u : 0u;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[0][e] = word_value(kind == 2u ? wi[e] : wa[e]);
+                    v[1][e] = word_value(wc[e]);
+                }
+            } else if (j == -1) {
+                kind = 2u;
+#pragma unroll
+                for (int e = 0; e < V; ++e) { v[0][e] = first[e]; v[1][e] = 0.f; }
             }
-            const bool all_inc = __all(inc), all_map = __all(map);
-            if (lane == 0) s_kind[wave] = all_inc ? 2u : all_map ? 1u : 0u;
-        } else if (lane == 0) {
-            s_kind[wave] = 0u;
+            if (kind)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    s.v[p][0][lane * V + e] = v[0][e];
+                    s.v[p][1][lane * V + e] = v[1][e];
+                }
+            if (lane == 0) s.kind[p] = kind;
         }
         __syncthreads();
-        int at = -1;
-#pragma unroll 1
-        for (int k = 0; k < NW; ++k) {
-            const uint32_t kind = s_kind[k];
-            if (kind == 2u) { at = k; break; }
-            if (kind == 0u) break;
-        }
-        if (at >= 0) {
+        const uint32_t kind = lane < reach * NW ? s.kind[lane] : 0u;
+        const uint64_t known = __ballot(kind == 2u), none = __ballot(kind == 0u);
+        const int at = known ? __builtin_ctzll(known) : 64;
+        if (at < (none ? __builtin_ctzll(none) : 64)) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) enter[e] = s_val[at][0][lane * V + e];
-#pragma unroll 1
+            for (int e = 0; e < V; ++e) enter[e] = s.v[at][0][lane * V + e];
+#pragma unroll 2
             for (int k = at - 1; k >= 0; --k)
 #pragma unroll
-                for (int e = 0; e < V; ++e)
-                    enter[e] = after(s_val[k][1][lane * V + e], enter[e], s_val[k][2][lane * V + e]);
+                for (int e = 0; e < V; ++e) enter[e] = after(s.v[k][0][lane * V + e], enter[e], s.v[k][1][lane * V + e]);
             return;
         }
         if (spin + 1 >= spin_max) {
@@ -191,63 +239,64 @@ __device__ __forceinline__ void look_back(const Words &wd, int64_t slot0, int64_
 }
 
 template <typename T, int V, bool kGate>
-__global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
+__global__ __launch_bounds__(kFwdWaves * 64, 4) void k_fwd(FwdArgs a) {
     typedef typename Raw<T, V>::type R;
     constexpr int NW = kFwdWaves, S = kChunk / NW, C = 64 * V;
     __shared__ uint64_t s_ticket;
     __shared__ float s_A[NW][C], s_c[NW][C];
-    __shared__ float s_val[NW][3][C];
-    __shared__ uint32_t s_kind[NW];
+    __shared__ Polled<V, NW> s_polled;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const Item it = take_item(a.ctl, a.B * a.G, a.tiles, a.G, &s_ticket);
-    const int64_t d0 = it.grp * C + lane * V;
+    const Item it = take_item(a.ctl, (uint32_t)a.B, (uint32_t)a.tiles, (uint32_t)a.G, &s_ticket);
+    const int64_t d0 = (int64_t)it.grp * C + lane * V;
     const bool live = d0 < a.D;      // (V divides D)
     const int64_t dl = live ? d0 : 0;
-    const int64_t t0 = it.tile * kChunk + wave * S;
-    const int n = (int)min((int64_t)S, a.L - t0);   // tokens of this wave, possibly none
+    const int64_t t0 = (int64_t)it.tile * kChunk + wave * S;
+    const int n = (int)max((int64_t)0, min((int64_t)S, a.L - t0));   // tokens of this wave
 
-    // rows past the end read the last token's (their maps are the identity)
-    const uint32_t lo = (uint32_t)(dl * sizeof(T));
-    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb;
-    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb;
-    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb;
+    const uint32_t lo = live ? (uint32_t)(d0 * sizeof(T)) : kOut;
+    const Rows rx = rows<T>(a.x, it.b * a.x_sb + t0 * a.x_st, a.x_st, n, a.D), rr = rows<T>(a.r, it.b * a.r_sb + t0 * a.r_st, a.r_st, n, a.D),
+               ri = rows<T>(a.i, it.b * a.i_sb + t0 * a.i_st, a.i_st, n, a.D);
     R vx[S], vr[S], vi[S], vz[kGate ? S : 1];
+    float A[V];   // of powers of two
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t t = min(t0 + s, a.L - 1);
-        vr[s] = row_load<R>(pr + t * a.r_st, lo);
-        vi[s] = row_load<R>(pi + t * a.i_st, lo);
-        vx[s] = row_load<R>(px + t * a.x_st, lo);
-    }
-    float A[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) A[e] = a.A[dl + e];
+    for (int e = 0; e < V; ++e) A[e] = a.A[dl + e] * kLog2e;
 
     float pa[S][V], ph[S][V];   // the map of the wave's tokens up to and with s
     float ca[V], ch[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { ca[e] = 1.f; ch[e] = 0.f; }
+    auto maps = [&](auto whole) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float at, wt;
-            decay(A[e] * sigmoid(get(vr[s], e)), at, wt);
-            const float bt = wt * sigmoid(get(vi[s], e)) * get(vx[s], e);
-            const float na = ca[e] * at, nh = fmaf(at, ch[e], bt);
-            ca[e] = s < n ? na : ca[e];
-            ch[e] = s < n ? nh : ch[e];
-            pa[s][e] = ca[e];
-            ph[s][e] = ch[e];
+        for (int s = 0; s < S; ++s) {
+            vr[s] = row_load<R>(rr, s, lo, whole);
+            vi[s] = row_load<R>(ri, s, lo, whole);
+            vx[s] = row_load<R>(rx, s, lo, whole);
         }
         fence();
-    }
-    if constexpr (kGate) {
-        const T *pz = static_cast<const T *>(a.z) + it.b * a.z_sb;
 #pragma unroll
-        for (int s = 0; s < S; ++s) vz[s] = row_load<R>(pz + min(t0 + s, a.L - 1) * a.z_st, lo);
-    }
+        for (int s = 0; s < S; ++s) {
+            if (decltype(whole)::value || s < n) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float l = A[e] * sigmoid(get(vr[s], e)), at = exp2_fast(l);
+                    const float wt = __builtin_amdgcn_sqrtf(one_minus_square(at, l));
+                    ca[e] *= at;
+                    ch[e] = fmaf(at, ch[e], wt * sigmoid(get(vi[s], e)) * get(vx[s], e));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) { pa[s][e] = ca[e]; ph[s][e] = ch[e]; }
+            fence();
+        }
+        if constexpr (kGate) {
+            const Rows rz = rows<T>(a.z, it.b * a.z_sb + t0 * a.z_st, a.z_st, n, a.D);
+#pragma unroll
+            for (int s = 0; s < S; ++s) vz[s] = row_load<R>(rz, s, lo, whole);
+        }
+    };
+    if (n >= S) maps(std::true_type{});
+    else maps(std::false_type{});
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         s_A[wave][lane * V + e] = ca[e];
@@ -270,11 +319,10 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
     }
     const int64_t slot0 = it.b * a.tiles * a.D, slot = slot0 + it.tile * a.D + d0;
     const bool last = it.tile == a.tiles - 1;
-    float enter[V];
-    if (it.tile == 0) {
+    float first[V], enter[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) enter[e] = a.init ? a.init[it.b * a.D + dl + e] : 0.f;
-    } else {
+    for (int e = 0; e < V; ++e) enter[e] = first[e] = a.init ? a.init[it.b * a.D + dl + e] : 0.f;
+    if (it.tile > 0) {
         if (!last && wave == 0 && live) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -283,7 +331,7 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
             }
         }
         look_back<V, NW>(Words{a.inc, a.mapA, a.mapC}, slot0, it.tile, a.D, d0, live, it.tag, a.ctl, a.spin_max, wave, lane,
-                         s_val, s_kind, enter);
+                         first, s_polled, enter);
     }
     if (wave == 0 && live) {
 #pragma unroll
@@ -294,22 +342,24 @@ __global__ __launch_bounds__(kFwdWaves * 64) void k_fwd(FwdArgs a) {
             if (a.states) a.states[slot + e] = enter[e];
         }
     }
-    if (!live) return;
     float hw[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) hw[e] = after(wA[e], enter[e], wc[e]);
-    T *py = static_cast<T *>(a.y) + (it.b * a.L + t0) * a.D;
+    const Rows ry = rows<T>(a.y, (it.b * a.L + t0) * a.D, a.D, n, a.D);
+    auto out = [&](auto whole) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        if (s >= n) continue;
-        float o[V];
+        for (int s = 0; s < S; ++s) {
+            float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            o[e] = fmaf(pa[s][e], hw[e], ph[s][e]);
-            if constexpr (kGate) o[e] *= silu(get(vz[s], e));
+            for (int e = 0; e < V; ++e) {
+                o[e] = fmaf(pa[s][e], hw[e], ph[s][e]);
+                if constexpr (kGate) o[e] *= silu(get(vz[s], e));
+            }
+            row_store<R>(ry, s, lo, put<T, V>(o), whole);
         }
-        row_store<R>(py + s * a.D, lo, put<T, V>(o));
-    }
+    };
+    if (n >= S) out(std::true_type{});
+    else out(std::false_type{});
 }
 
 // Gradients.  With dh_t = dy_t [SiLU(z_t)], q_t = a_t (dh_t + q_{t+1}) (q_L =
@@ -325,69 +375,79 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     constexpr int NW = kBwdWaves, S = kChunk / NW, C = 64 * V;
     __shared__ uint64_t s_ticket;
     __shared__ float s_A[NW][C], s_c[NW][C], s_q[NW][C];
-    __shared__ float s_val[NW][3][C];
-    __shared__ uint32_t s_kind[NW];
+    __shared__ Polled<V, NW> s_polled;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const Item it = take_item(a.ctl, a.B * a.G, a.tiles, a.G, &s_ticket);
-    const int64_t tile = a.tiles - 1 - it.tile;    // in token order; it.tile counts from the end
-    const int64_t d0 = it.grp * C + lane * V;
+    const Item it = take_item(a.ctl, (uint32_t)a.B, (uint32_t)a.tiles, (uint32_t)a.G, &s_ticket);
+    const int tile = (int)a.tiles - 1 - it.tile;    // in token order; it.tile counts from the end
+    const int64_t d0 = (int64_t)it.grp * C + lane * V;
     const bool live = d0 < a.D;
     const int64_t dl = live ? d0 : 0;
-    const int64_t t0 = tile * kChunk + wave * S;
-    const int n = (int)min((int64_t)S, a.L - t0);
+    const int64_t t0 = (int64_t)tile * kChunk + wave * S;
+    const int n = (int)max((int64_t)0, min((int64_t)S, a.L - t0));
 
-    const uint32_t lo = (uint32_t)(dl * sizeof(T));
-    const T *px = static_cast<const T *>(a.x) + it.b * a.x_sb;
-    const T *pr = static_cast<const T *>(a.r) + it.b * a.r_sb;
-    const T *pi = static_cast<const T *>(a.i) + it.b * a.i_sb;
-    const T *pd = static_cast<const T *>(a.dy) + it.b * a.L * a.D;
+    const uint32_t lo = live ? (uint32_t)(d0 * sizeof(T)) : kOut;
+    const int64_t orow = (it.b * a.L + t0) * a.D;
+    const Rows rx = rows<T>(a.x, it.b * a.x_sb + t0 * a.x_st, a.x_st, n, a.D), rr = rows<T>(a.r, it.b * a.r_sb + t0 * a.r_st, a.r_st, n, a.D),
+               ri = rows<T>(a.i, it.b * a.i_sb + t0 * a.i_st, a.i_st, n, a.D), rd = rows<T>(a.dy, orow, a.D, n, a.D);
     R vx[S], vr[S], vi[S], vd[S], vz[kGate ? S : 1];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t t = min(t0 + s, a.L - 1);
-        vr[s] = row_load<R>(pr + t * a.r_st, lo);
-        vi[s] = row_load<R>(pi + t * a.i_st, lo);
-        vx[s] = row_load<R>(px + t * a.x_st, lo);
-        vd[s] = row_load<R>(pd + t * a.D, lo);
-        if constexpr (kGate) vz[s] = row_load<R>(static_cast<const T *>(a.z) + it.b * a.z_sb + t * a.z_st, lo);
-    }
-    float A[V], enter[V];
+    float A[V], A2[V], enter[V];   // (A2: of powers of two)
     const int64_t srow = (it.b * a.tiles + tile) * a.D;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         A[e] = a.A[dl + e];
+        A2[e] = A[e] * kLog2e;
         enter[e] = a.states[srow + dl + e];
     }
     // the wave's maps: of the state (A, c) from its first token to its last, of
     // the gradient (A, q) from its last to its first
-    float at[S][V], bt[S][V];
+    float at[S][V], bt[S][V], rho[S][V], iota[S][V];
     float cA[V], cc[V], cq[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { cA[e] = 1.f; cc[e] = 0.f; cq[e] = 0.f; }
+    auto maps = [&](auto whole) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
+        for (int s = 0; s < S; ++s) {
+            vr[s] = row_load<R>(rr, s, lo, whole);
+            vi[s] = row_load<R>(ri, s, lo, whole);
+            vx[s] = row_load<R>(rx, s, lo, whole);
+            vd[s] = row_load<R>(rd, s, lo, whole);
+        }
+        if constexpr (kGate) {
+            const Rows rz = rows<T>(a.z, it.b * a.z_sb + t0 * a.z_st, a.z_st, n, a.D);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float wt;
-            decay(A[e] * sigmoid(get(vr[s], e)), at[s][e], wt);
-            bt[s][e] = wt * sigmoid(get(vi[s], e)) * get(vx[s], e);
-            if (s >= n) { at[s][e] = 1.f; bt[s][e] = 0.f; }
-            cA[e] *= at[s][e];
-            cc[e] = fmaf(at[s][e], cc[e], bt[s][e]);
+            for (int s = 0; s < S; ++s) vz[s] = row_load<R>(rz, s, lo, whole);
         }
         fence();
-    }
 #pragma unroll
-    for (int s = S - 1; s >= 0; --s) {
+        for (int s = 0; s < S; ++s) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float dh = get(vd[s], e);
-            if constexpr (kGate) dh *= silu(get(vz[s], e));
-            cq[e] = s < n ? at[s][e] * (dh + cq[e]) : cq[e];
+            for (int e = 0; e < V; ++e) {
+                rho[s][e] = sigmoid(get(vr[s], e));
+                iota[s][e] = sigmoid(get(vi[s], e));
+                const float l = A2[e] * rho[s][e];
+                at[s][e] = exp2_fast(l);
+                bt[s][e] = __builtin_amdgcn_sqrtf(one_minus_square(at[s][e], l)) * iota[s][e] * get(vx[s], e);
+                if (!decltype(whole)::value && s >= n) { at[s][e] = 1.f; bt[s][e] = 0.f; }
+                cA[e] *= at[s][e];
+                cc[e] = fmaf(at[s][e], cc[e], bt[s][e]);
+            }
+            fence();
         }
-        fence();
-    }
+#pragma unroll
+        for (int s = S - 1; s >= 0; --s) {
+            if (!decltype(whole)::value && s >= n) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float dh = get(vd[s], e);
+                if constexpr (kGate) dh *= silu(get(vz[s], e));
+                cq[e] = at[s][e] * (dh + cq[e]);
+            }
+            fence();
+        }
+    };
+    if (n >= S) maps(std::true_type{});
+    else maps(std::false_type{});
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         s_A[wave][lane * V + e] = cA[e];
@@ -424,11 +484,10 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
 
     const int64_t slot0 = it.b * a.tiles * a.D, slot = slot0 + it.tile * a.D + d0;
     const bool last = it.tile == a.tiles - 1;
-    float q[V];
-    if (it.tile == 0) {
+    float first[V], q[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) q[e] = a.dfinal ? a.dfinal[it.b * a.D + dl + e] : 0.f;
-    } else {
+    for (int e = 0; e < V; ++e) q[e] = first[e] = a.dfinal ? a.dfinal[it.b * a.D + dl + e] : 0.f;
+    if (it.tile > 0) {
         if (!last && wave == 0 && live) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -437,7 +496,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
             }
         }
         look_back<V, NW>(Words{a.inc, a.mapA, a.mapC}, slot0, it.tile, a.D, d0, live, it.tag, a.ctl, a.spin_max, wave, lane,
-                         s_val, s_kind, q);
+                         first, s_polled, q);
     }
     if (wave == 0 && live) {
 #pragma unroll
@@ -450,44 +509,40 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     float dA[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { q[e] = after(wA[e], q[e], wq[e]); dA[e] = 0.f; }
-    const int64_t orow = (it.b * a.L + t0) * a.D;
+    const Rows wx = rows<T>(a.dx, orow, a.D, n, a.D), wr = rows<T>(a.dr, orow, a.D, n, a.D), wi = rows<T>(a.di, orow, a.D, n, a.D);
+    const Rows wz = rows<T>(kGate ? a.dz : a.dx, orow, a.D, n, a.D);
 #pragma unroll
     for (int s = S - 1; s >= 0; --s) {
         if (s >= n) continue;
-        forget(vr[s]);
-        forget(vi[s]);
         forget(vx[s]);
         forget(vd[s]);
         float ox[V], orr[V], oi[V], oz[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float x = get(vx[s], e), dy = get(vd[s], e);
-            const float rho = sigmoid(get(vr[s], e)), iota = sigmoid(get(vi[s], e));
-            float av, w;
-            decay(A[e] * rho, av, w);
+            const float x = get(vx[s], e), dy = get(vd[s], e), av = at[s][e], ig = iota[s][e];
+            forget(rho[s][e]);   // (w is formed again)
+            const float om = one_minus_square(av, A2[e] * rho[s][e]);
+            const float iw = om > 0.f ? __builtin_amdgcn_rsqf(om) : 0.f, w = om * iw;
             float dh = dy;
             if constexpr (kGate) {
                 const float z = get(vz[s], e), sz = sigmoid(z), gz = z * sz;
                 dh = dy * gz;
-                const float hv = fmaf(av, bt[s][e], w * iota * x);
+                const float hv = fmaf(av, bt[s][e], w * ig * x);
                 oz[e] = dy * hv * fmaf(gz, 1.f - sz, sz);
             }
-            const float g = dh + q[e], gi = g * iota;
+            const float g = dh + q[e], gi = g * ig;
             q[e] = av * g;
             ox[e] = gi * w;
-            oi[e] = ox[e] * x * (1.f - iota);
-            const float ratio = w > 0.f ? av * av * __builtin_amdgcn_rcpf(w) : 0.f;
-            const float dl_ = fmaf(q[e], bt[s][e], -ratio * (gi * x));
-            const float rd = rho * dl_;
-            orr[e] = A[e] * rd * (1.f - rho);
-            dA[e] += rd;
+            oi[e] = ox[e] * x * (1.f - ig);
+            const float dl_ = fmaf(q[e], bt[s][e], -(av * av * iw) * (gi * x));
+            const float rl = rho[s][e] * dl_;
+            orr[e] = A[e] * rl * (1.f - rho[s][e]);
+            dA[e] += rl;
         }
-        if (live) {
-            row_store<R>(static_cast<T *>(a.dx) + orow + s * a.D, lo, put<T, V>(ox));
-            row_store<R>(static_cast<T *>(a.dr) + orow + s * a.D, lo, put<T, V>(orr));
-            row_store<R>(static_cast<T *>(a.di) + orow + s * a.D, lo, put<T, V>(oi));
-            if constexpr (kGate) row_store<R>(static_cast<T *>(a.dz) + orow + s * a.D, lo, put<T, V>(oz));
-        }
+        row_store<R>(wx, s, lo, put<T, V>(ox), std::true_type{});
+        row_store<R>(wr, s, lo, put<T, V>(orr), std::true_type{});
+        row_store<R>(wi, s, lo, put<T, V>(oi), std::true_type{});
+        if constexpr (kGate) row_store<R>(wz, s, lo, put<T, V>(oz), std::true_type{});
         fence();
     }
     // the tile's part of dA (tagged like every word of the workspace)
@@ -546,8 +601,8 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
     float h[V], o[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        float at, w;
-        decay(a.A[d + e] * sigmoid(get(vr, e)), at, w);
+        const float l = a.A[d + e] * kLog2e * sigmoid(get(vr, e)), at = exp2_fast(l);
+        const float w = __builtin_amdgcn_sqrtf(one_minus_square(at, l));
         h[e] = fmaf(at, ps[e], w * sigmoid(get(vi, e)) * get(vx, e));
         o[e] = h[e];
         if constexpr (kGate) o[e] *= silu(get(vz, e));
@@ -566,7 +621,8 @@ template <typename T, int V> hipError_t fwd(const FwdArgs &a, hipStream_t s) {
 template <typename T, int V> hipError_t bwd(const BwdArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)(a.B * a.G * a.tiles)), block(kBwdWaves * 64);
     if (a.z) k_bwd<T, V, true><<<grid, block, 0, s>>>(a);
-    else k_bwd<T, V, false><<<grid, block, 0, s>>>(a);
+    else if constexpr (V == 1) k_bwd<T, V, false><<<grid, block, 0, s>>>(a);   // (bwd_channels)
+    else return hipErrorInvalidValue;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     k_sum<<<dim3((unsigned)((a.D + 63) / 64)), dim3(64 * kSumRows), 0, s>>>(a.part, a.B * a.tiles, a.D, a.dA);

@@ -57,6 +57,9 @@ m3_status check_glr(const m3_glr_dims *d, bool step) {
     if (d->batch > INT_MAX || d->width > INT_MAX || d->batch * d->width > kMost / L) return M3_ERR_SHAPE;
     for (int64_t s : strides)
         if (s < 0 || s > kMost / std::max(L, d->batch)) return M3_ERR_SHAPE;
+    // a workgroup's rows within 31-bit offsets
+    for (int64_t s : {d->width, d->x_stride_t, d->r_stride_t, d->i_stride_t, d->z_stride_t})
+        if (!step && s > (INT64_C(1) << 23)) return M3_ERR_SHAPE;
     if (step) return d->batch * d->width / 256 < kMostGroups ? M3_OK : M3_ERR_SHAPE;
     // one workgroup a tile (groups of 64 channels: the most)
     const int64_t tiles = (d->seqlen + glr::kChunk - 1) / glr::kChunk, groups = (d->width + 63) / 64;
@@ -143,6 +146,7 @@ extern "C" m3_status m3_glr_bwd(const m3_glr_dims *d, const void *x, const void 
     if (!aligned(workspace, 16)) return M3_ERR_ALIGN;
     const GlrLayout w = glr_layout(d);
     if (!workspace || workspace_bytes < w.total) return M3_ERR_WORKSPACE;
+    V = glr::bwd_channels(V, z != nullptr);
     glr::BwdArgs a = {};
     glr_common(d, x, r, i, A, z, V, workspace, &a);
     a.dy = dy; a.states = states; a.dfinal = dfinal;
