@@ -561,38 +561,57 @@ def scan_bwd(x, Bm, Cm, dt, A, lam, theta, D, dy, chunk: int, dfinal=None, init_
 # Gated linear recurrence
 # ---------------------------------------------------------------------------
 
-def _rows(t: Optional[torch.Tensor], like: torch.Tensor, name: str):
-    """A pointer and the batch and token strides of a tensor shaped and typed like
-    `like` whose channels lie next to each other."""
-    if t is None:
-        return None, 0, 0
-    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must have the shape, dtype and device of x")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
-    # (a stride over one element is never walked, whatever torch reports)
-    st = [t.stride(k) if t.shape[k] > 1 else 0 for k in range(t.dim() - 1)]
-    return t.data_ptr(), st[0], (st[1] if len(st) > 1 else 0)
+def _meta(t: Optional[torch.Tensor]):
+    """What the checks of a tensor go by."""
+    return None if t is None else (t.shape, t.dtype, t.device, t.stride())
+
+
+def _empty(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _f32(t: Optional[torch.Tensor], shape, dev, name: str):
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != torch.float32 or t.device != dev:
-        raise ValueError(f"{name} must be fp32 {tuple(shape)} on {dev}")
-    return _p(t)
+    if t.shape != shape or t.dtype is not torch.float32 or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous fp32 {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, shape, dtype, dev, name: str):
+    if t.shape != shape or t.dtype is not dtype or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=256)
+def _glr_dims(x, r, i, z) -> M3GlrDims:
+    """The dims of a recurrence by the tensors' shapes, types and strides, checked (a
+    program makes the same ones again and again; the library only reads them)."""
+    shape, dtype = x[0], x[1]
+    if dtype not in _IO:
+        raise ValueError("x must be fp32 or bf16")
+    if len(shape) not in (2, 3):
+        raise ValueError(f"x must be [B, L, D] or [B, D], got {tuple(shape)}")
+    strides = []
+    for name, t in (("x", x), ("r", r), ("i", i), ("z", z)):
+        if t is None:
+            strides += [0, 0]
+            continue
+        if t[:3] != x[:3]:
+            raise ValueError(f"{name} must have the shape, dtype and device of x")
+        if shape[-1] > 1 and t[3][-1] != 1:
+            raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
+        # (a stride over one element is never walked, whatever torch reports)
+        st = [t[3][k] if shape[k] > 1 else 0 for k in range(len(shape) - 1)]
+        strides += [st[0], st[1] if len(st) > 1 else 0]
+    return M3GlrDims(shape[0], 1 if len(shape) == 2 else shape[1], shape[-1], _IO[dtype], 0, *strides)
 
 
 def glr_dims(x, r=None, i=None, z=None) -> M3GlrDims:
     """The dims of a recurrence over x [B, L, D] (a step: [B, D]) with gates r and i
     and the output gate z."""
-    if x.dtype not in _IO:
-        raise ValueError("x must be fp32 or bf16")
-    step = x.dim() == 2
-    if x.dim() not in (2, 3):
-        raise ValueError(f"x must be [B, L, D] or [B, D], got {tuple(x.shape)}")
-    s = [v for name, t in (("x", x), ("r", r), ("i", i), ("z", z)) for v in _rows(t, x, name)[1:]]
-    return M3GlrDims(x.shape[0], 1 if step else x.shape[1], x.shape[-1], _IO[x.dtype], 0, *s)
+    return M3GlrDims.from_buffer_copy(_glr_dims(_meta(x), _meta(r), _meta(i), _meta(z)))   # (the caller's own)
 
 
 def glr_workspace(x, r=None, i=None, z=None) -> torch.Tensor:
@@ -618,21 +637,22 @@ def glr_fwd(x, r, i, A, z=None, init_state=None, save_states: bool = False, out=
     fp32, channels next to each other, any batch and token strides), A [D] fp32.
     Returns y [B, L, D], final_state [B, D] fp32 and, with `save_states`, the states
     that glr_bwd takes.  `out` may supply (y, final_state)."""
-    d = glr_dims(x, r, i, z)
-    B, L, D = x.shape
-    f32 = dict(dtype=torch.float32, device=x.device)
-    y, fs = out if out is not None else (torch.empty((B, L, D), dtype=x.dtype, device=x.device),
-                                         torch.empty((B, D), **f32))
-    if y.shape != x.shape or y.dtype != x.dtype:
-        raise ValueError("y must have the shape and dtype of x")
-    states = torch.empty((B, -(-L // GLR_CHUNK), D), **f32) if save_states else None
+    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    B, L, D = shape
+    if out is None:
+        y = _empty(x)
+        fs = torch.empty((B, D), dtype=torch.float32, device=dev)
+    else:
+        y, fs = out
+    states = torch.empty((B, -(-L // GLR_CHUNK), D), dtype=torch.float32, device=dev) if save_states else None
     if workspace is None:
         workspace = glr_workspace(x, r, i, z)
     _check(lib().m3_glr_fwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
-                            _f32(A, (D,), x.device, "A"), None if z is None else z.data_ptr(),
-                            _f32(init_state, (B, D), x.device, "init_state"), _p(y),
-                            _f32(fs, (B, D), x.device, "final_state"), _p(states), _p(workspace),
-                            workspace.numel(), _stream(stream)))
+                            _f32(A, (D,), dev, "A"), None if z is None else z.data_ptr(),
+                            _f32(init_state, (B, D), dev, "init_state"),
+                            _like(y, shape, dtype, dev, "y"), _f32(fs, (B, D), dev, "final_state"),
+                            _p(states), _p(workspace), workspace.numel(), _stream(stream)))
     return (y, fs, states) if save_states else (y, fs)
 
 
@@ -641,22 +661,23 @@ def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = Fals
     """m3_glr_bwd: gradients of J = <dy, y> + <dfinal, final_state>, from the forward's
     inputs and the states it saved.  Returns a dict: dx, dr, di (dz) in the io dtype,
     dA [D] fp32 and, with `want_dinit`, dinit [B, D] fp32."""
-    d = glr_dims(x, r, i, z)
-    B, L, D = x.shape
-    if dy.shape != x.shape or dy.dtype != x.dtype:
-        raise ValueError("dy must have the shape and dtype of x")
-    out = {k: torch.empty((B, L, D), dtype=x.dtype, device=x.device)
-           for k in ("dx", "dr", "di") + (("dz",) if z is not None else ())}
-    out["dA"] = torch.empty((D,), dtype=torch.float32, device=x.device)
+    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    B, L, D = shape
+    out = {k: _empty(x)
+           for k in (("dx", "dr", "di") if z is None else ("dx", "dr", "di", "dz"))}
+    out["dA"] = torch.empty((D,), dtype=torch.float32, device=dev)
     if want_dinit:
-        out["dinit"] = torch.empty((B, D), dtype=torch.float32, device=x.device)
+        out["dinit"] = torch.empty((B, D), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = glr_workspace(x, r, i, z)
     _check(lib().m3_glr_bwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
-                            _f32(A, (D,), x.device, "A"), None if z is None else z.data_ptr(),
-                            _f32(states, (B, -(-L // GLR_CHUNK), D), x.device, "states"), _p(dy),
-                            _f32(dfinal, (B, D), x.device, "dfinal"), _p(out["dx"]), _p(out["dr"]),
-                            _p(out["di"]), _p(out.get("dz")), _p(out["dA"]), _p(out.get("dinit")),
+                            _f32(A, (D,), dev, "A"), None if z is None else z.data_ptr(),
+                            _f32(states, (B, -(-L // GLR_CHUNK), D), dev, "states"),
+                            _like(dy, shape, dtype, dev, "dy"), _f32(dfinal, (B, D), dev, "dfinal"),
+                            out["dx"].data_ptr(), out["dr"].data_ptr(), out["di"].data_ptr(),
+                            None if z is None else out["dz"].data_ptr(), out["dA"].data_ptr(),
+                            out["dinit"].data_ptr() if want_dinit else None,
                             _p(workspace), workspace.numel(), _stream(stream)))
     return out
 
@@ -664,16 +685,16 @@ def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = Fals
 def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
     """m3_glr_step: one token, x, r, i, z [B, D]; advances `state` [B, D] fp32 in
     place and returns y [B, D]."""
-    d = glr_dims(x, r, i, z)
-    if x.dim() != 2:
-        raise ValueError(f"x must be [B, D], got {tuple(x.shape)}")
+    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    if len(shape) != 2:
+        raise ValueError(f"x must be [B, D], got {tuple(shape)}")
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    elif y.shape != x.shape or y.dtype != x.dtype:
-        raise ValueError("y must have the shape and dtype of x")
-    _check(lib().m3_glr_step(ctypes.byref(d), _f32(state, x.shape, x.device, "state"), x.data_ptr(),
-                             r.data_ptr(), i.data_ptr(), _f32(A, x.shape[1:], x.device, "A"),
-                             None if z is None else z.data_ptr(), _p(y), _stream(stream)))
+        y = _empty(x)
+    _check(lib().m3_glr_step(ctypes.byref(d), _f32(state, shape, dev, "state"), x.data_ptr(),
+                             r.data_ptr(), i.data_ptr(), _f32(A, shape[1:], dev, "A"),
+                             None if z is None else z.data_ptr(), _like(y, shape, dtype, dev, "y"),
+                             _stream(stream)))
     return y
 
 
@@ -681,71 +702,71 @@ def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
 # Gated feed-forward block
 # ---------------------------------------------------------------------------
 
-def _ffn_rows(t: torch.Tensor, name: str) -> torch.Tensor:
-    """[..., D] as rows [T, D] (a view)."""
-    t = t if t.dim() == 2 else t.view(-1, t.shape[-1])
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
-    return t
-
-
-def _ffn_dims(x, Wg, act="silu", dy=None) -> M3FfnDims:
-    if x.dtype not in _IO:
+@functools.lru_cache(maxsize=256)
+def _ffn_dims(x, Wg, Wu, Wd, dy, act) -> M3FfnDims:
+    """The dims of a block by the tensors' shapes, types and strides, checked."""
+    shape, dtype, dev, strides = x
+    if dtype not in _IO:
         raise ValueError("x must be fp32 or bf16")
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}")
-    T, D = x.shape
-    F = Wg.shape[0]
-    # (the stride of a single row is never walked, whatever torch reports)
-    st = [t.stride(0) if t is not None and T > 1 else D for t in (x, dy)]
-    return M3FfnDims(T, D, F, _IO[x.dtype], _ACT[act], *st)
+    D, F = shape[-1], Wg[0][0]
+    for name, t, want in (("Wg", Wg, (F, D)), ("Wu", Wu, (F, D)), ("Wd", Wd, (D, F))):
+        if t is not None and (t[0] != want or t[1] != dtype or t[2] != dev):
+            raise ValueError(f"{name} must be {dtype} {want} on {dev}")
+    rows = []
+    for name, t in (("x", x), ("dy", dy)):
+        if t is None:
+            rows.append(D)
+            continue
+        if t[:3] != x[:3]:
+            raise ValueError(f"{name} must have the shape, dtype and device of x")
+        st = t[3]
+        if D > 1 and st[-1] != 1:
+            raise ValueError(f"{name}: libm3 takes channels next to each other (channel stride 1)")
+        # [..., D] as rows of one stride (a stride over one element is never walked)
+        dims = [(n, st[k]) for k, n in enumerate(shape[:-1]) if n > 1]
+        for (_, outer), (n, inner) in zip(dims, dims[1:]):
+            if outer != n * inner:
+                raise ValueError(f"{name}: rows must lie at one stride")
+        rows.append(dims[-1][1] if dims else D)
+    T = 1
+    for n in shape[:-1]:
+        T *= n
+    return M3FfnDims(T, D, F, _IO[dtype], _ACT[act], *rows)
 
 
 def ffn_workspace(x, Wg, backward: bool = False) -> torch.Tensor:
     """A workspace for ffn_fwd (ffn_bwd with `backward`, which serves both) of x
     [..., D] and Wg [F, D]: keep it for further calls, one at a time."""
-    d = _ffn_dims(_ffn_rows(x, "x"), Wg)
+    d = _ffn_dims(_meta(x), _meta(Wg), None, None, None, "silu")
     n = int(lib().m3_ffn_workspace_bytes(ctypes.byref(d), int(backward)))
     return torch.empty(max(n, 16), dtype=torch.uint8, device=x.device)
 
 
-def _ffn_check(x, Wg, Wu, Wd):
-    D, F = x.shape[-1], Wg.shape[0]
-    for name, t, shape in (("Wg", Wg, (F, D)), ("Wu", Wu, (F, D)), ("Wd", Wd, (D, F))):
-        if tuple(t.shape) != shape or t.dtype != x.dtype or t.device != x.device:
-            raise ValueError(f"{name} must be {x.dtype} {shape} on {x.device}")
-
-
 def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=None):
-    """m3_ffn_fwd: y = (act(x Wg^T) o (x Wu^T)) Wd^T; x [..., D] (rows of [T, D] may be
-    strided), Wg and Wu [F, D], Wd [D, F], bf16 or fp32; act "silu" or "gelu" (tanh
-    form).  Returns y, shaped like x."""
-    _ffn_check(x, Wg, Wu, Wd)
-    rows = _ffn_rows(x, "x")
-    d = _ffn_dims(rows, Wg, act)
-    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if y.shape != x.shape or y.dtype != x.dtype:
-        raise ValueError("y must have the shape and dtype of x")
+    """m3_ffn_fwd: y = (act(x Wg^T) o (x Wu^T)) Wd^T; x [..., D] (rows at one stride), Wg
+    and Wu [F, D], Wd [D, F], bf16 or fp32; act "silu" or "gelu" (tanh form).  Returns
+    y, shaped like x, contiguous."""
+    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), None, act)
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    y = out if out is not None else _empty(x)
     if workspace is None:
         workspace = ffn_workspace(x, Wg)
-    _check(lib().m3_ffn_fwd(ctypes.byref(d), rows.data_ptr(), _p(Wg), _p(Wu), _p(Wd), _p(y), _p(workspace),
-                            workspace.numel(), _stream(stream)))
+    _check(lib().m3_ffn_fwd(ctypes.byref(d), x.data_ptr(), _p(Wg), _p(Wu), _p(Wd),
+                            _like(y, shape, dtype, dev, "y"), _p(workspace), workspace.numel(),
+                            _stream(stream)))
     return y
 
 
 def ffn_bwd(x, Wg, Wu, Wd, dy, act: str = "silu", workspace=None, stream=None):
     """m3_ffn_bwd: gradients of J = <dy, y> from the forward's inputs (g and u are formed
     again).  Returns a dict: dx (shaped like x), dWg, dWu, dWd, in the io dtype."""
-    _ffn_check(x, Wg, Wu, Wd)
-    if dy.shape != x.shape or dy.dtype != x.dtype:
-        raise ValueError("dy must have the shape and dtype of x")
-    rows, drows = _ffn_rows(x, "x"), _ffn_rows(dy, "dy")
-    d = _ffn_dims(rows, Wg, act, drows)
-    out = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device), dWg=torch.empty_like(Wg),
-               dWu=torch.empty_like(Wu), dWd=torch.empty_like(Wd))
+    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), _meta(dy), act)
+    out = dict(dx=_empty(x), dWg=_empty(Wg), dWu=_empty(Wu), dWd=_empty(Wd))
     if workspace is None:
         workspace = ffn_workspace(x, Wg, backward=True)
-    _check(lib().m3_ffn_bwd(ctypes.byref(d), rows.data_ptr(), _p(Wg), _p(Wu), _p(Wd), drows.data_ptr(),
+    _check(lib().m3_ffn_bwd(ctypes.byref(d), x.data_ptr(), _p(Wg), _p(Wu), _p(Wd), dy.data_ptr(),
                             _p(out["dx"]), _p(out["dWg"]), _p(out["dWu"]), _p(out["dWd"]), _p(workspace),
                             workspace.numel(), _stream(stream)))
     return out
