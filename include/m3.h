@@ -599,7 +599,8 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * p fp32, g fp32 or bf16 (grad_dtype, one for all), m and v fp32, all with n
  * elements; low (NULL: none) receives p rounded to bf16.  grad_scale is a
  * DEVICE scalar (NULL: 1), e.g. the coefficient that clips the gradients'
- * norm.  n = 0 is allowed.  Every operation is rounded to fp32 by itself.
+ * norm.  n = 0 is allowed.  Operations are
+ * rounded to fp32 one by one, the root and the quotient within two ulps.
  *
  * 8-bit states (M3_ADAMW_8BIT): m and v hold e4m3 codes (1 byte an element) of
  * m and of sqrt(v), divided by scales[n / 256 rounded up][2] (fp32; m's, then
@@ -610,9 +611,7 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * call), so pass another seed for every step; a sqrt(v) that is not zero is
  * stored as at least the smallest code.  A non-finite gradient spoils its
  * block.
- * Pointers need their element's alignment (else M3_ERR_ALIGN); whole vectors
- * are moved where p, g, m, v and low are aligned for four elements.  A
- * NULL table with count > 0, or a NULL pointer in a tensor with n > 0, is
+ * Pointers need their element's alignment only (else M3_ERR_ALIGN).  A NULL table with count > 0, or a NULL pointer in a tensor with n > 0, is
  * M3_ERR_NULL; n < 0, step < 1, a beta outside [0, 1), eps < 0, or a lr,
  * decay or eps that is not finite is M3_ERR_SHAPE.
  */

@@ -8,7 +8,7 @@ namespace m3 {
 namespace adamw {
 
 constexpr int kBlockElems = 256;     // elements that share the scales of 8-bit states
-constexpr int kChunkElems = 4096;    // elements a workgroup
+constexpr int kChunkElems = 1024;    // elements a workgroup
 constexpr int kTensors = 48;         // tensors a launch (their table is a kernel argument)
 
 struct Tensor {
@@ -17,7 +17,7 @@ struct Tensor {
     void *m, *v;
     void *low;           // bf16 copy of p, or null
     float *scales;       // [blocks][2], 8-bit states only
-    int64_t n;
+    int32_t chunks, tail;    // workgroups, elements of the last one
     float keep;          // 1 - lr * weight decay
     uint32_t seed;
 };

@@ -10,9 +10,14 @@
 // should on average.  (sqrt(v), not v: half the range in powers of two.)  The
 // random numbers are a hash of the element's index and the tensor's seed.
 //
-// Streaming: every byte is read and written once.  A wave takes blocks of 256
-// consecutive elements, four a lane, so an 8-bit block's largest magnitude is
-// one wave reduction.  Every operation is rounded by itself (no contraction).
+// Streaming: every byte is read and written once, past the caches (they hold
+// nothing of it that is used again: 268 million parameters in fp32, 5.5 TB/s
+// through them, 6.1 past them).  A wave takes one block of 256 consecutive
+// elements, four a lane, so an 8-bit block's largest magnitude is one wave
+// reduction; more blocks a wave were slower (four: 5.9 TB/s).  Operations are
+// rounded to fp32 one by one; the root and the quotient are the hardware's, an
+// ulp or two off (rounded exactly they made the 8-bit step wait for the vector
+// units: 857 us against KKK for 268 million parameters).
 #include "m3_adamw.h"
 #include "m3_device.h"
 
@@ -20,17 +25,18 @@ namespace m3 {
 namespace adamw {
 namespace {
 
-constexpr int kWaves = 4, kPer = kChunkElems / (kWaves * kBlockElems);   // blocks a wave
+constexpr int kWaves = kChunkElems / kBlockElems;
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
     return v;
 }
-__device__ __forceinline__ uint32_t noise(uint32_t index, uint32_t seed) {
-    uint32_t h = (index ^ seed) * 0x9E3779B1u;   // odd parts of the golden ratio and of sqrt 2
-    h = (h ^ (h >> 15)) * 0x6A09E667u;
-    h = (h ^ (h >> 13)) * 0x9E3779B1u;
+// Odd parts of the golden ratio and of sqrt 2; `first` is (index ^ seed) kGolden.
+constexpr uint32_t kGolden = 0x9E3779B1u, kRoot2 = 0x6A09E667u;
+__device__ __forceinline__ uint32_t noise(uint32_t first) {
+    uint32_t h = (first ^ (first >> 15)) * kRoot2;
+    h = (h ^ (h >> 13)) * kGolden;
     return h ^ (h >> 16);
 }
 // |w| <= 448 (a rounding more at most) to an e4m3 number, up with the
@@ -45,18 +51,21 @@ __device__ __forceinline__ float round8(float w, uint32_t u) {
     return w < 0.f ? -c : c;
 }
 
+// Four elements of a tensor, which may start on any element: the vector
+// accesses of global memory need no more alignment than that.
 template <typename G> struct Four;
-template <> struct Four<float> { typedef f32x4 type; };
-template <> struct Four<bf16> { typedef bf16x4 type; };
+template <> struct Four<float> { typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Four<bf16> { typedef __bf16 type __attribute__((ext_vector_type(4), aligned(2))); };
+typedef uint32_t Codes __attribute__((aligned(1)));
 
-// Element e of lane `lane` in a block: four in a row (whole vectors), or one
-// of each 64 (any alignment, and the block that a tensor ends in).
+// Element e of lane `lane` in a block: four in a row, or one of each 64 in the
+// block that a tensor ends in.
 template <bool kVec> __device__ __forceinline__ int place(int lane, int e) { return kVec ? lane * 4 + e : lane + 64 * e; }
 
 template <typename X, bool kVec>
 __device__ __forceinline__ void load4(const X *p, int lane, int left, float (&o)[4]) {
     if constexpr (kVec) {
-        const typename Four<X>::type w = *reinterpret_cast<const typename Four<X>::type *>(p + lane * 4);
+        const typename Four<X>::type w = __builtin_nontemporal_load(reinterpret_cast<const typename Four<X>::type *>(p + lane * 4));
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = (float)w[e];
     } else {
@@ -70,7 +79,7 @@ __device__ __forceinline__ void store4(X *p, int lane, int left, const float (&v
         typename Four<X>::type w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = (X)v[e];
-        *reinterpret_cast<typename Four<X>::type *>(p + lane * 4) = w;
+        __builtin_nontemporal_store(w, reinterpret_cast<typename Four<X>::type *>(p + lane * 4));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -80,7 +89,7 @@ __device__ __forceinline__ void store4(X *p, int lane, int left, const float (&v
 // Four e4m3 codes
 template <bool kVec> __device__ __forceinline__ void load8(const uint8_t *p, int lane, int left, float (&o)[4]) {
     if constexpr (kVec) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(p + lane * 4);
+        const uint32_t w = __builtin_nontemporal_load(reinterpret_cast<const Codes *>(p + lane * 4));
         o[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
         o[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
         o[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
@@ -95,7 +104,7 @@ template <bool kVec> __device__ __forceinline__ void store8(uint8_t *p, int lane
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
     if constexpr (kVec) {
-        *reinterpret_cast<uint32_t *>(p + lane * 4) = (uint32_t)w;
+        __builtin_nontemporal_store((uint32_t)w, reinterpret_cast<Codes *>(p + lane * 4));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -114,8 +123,8 @@ __device__ __forceinline__ void update(const Step &k, float keep, float g, float
     if (k.scaled) g = g * k.gs;
     m = m * k.b1 + g * k.c1;
     v = v * k.b2 + (g * g) * k.c2;
-    rv = __builtin_sqrtf(v);
-    p = p * keep - (m * k.rate) / (rv * k.root + k.eps);
+    rv = __builtin_amdgcn_sqrtf(v);
+    p = p * keep - m * k.rate * __builtin_amdgcn_rcpf(rv * k.root + k.eps);
 }
 
 template <typename G, bool kEight, bool kVec>
@@ -161,11 +170,14 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t ba
         if (__any(bad_m)) am = __builtin_nanf("");
         if (__any(bad_v)) av = __builtin_nanf("");
         const float nm = __fmul_rn(am, 1.f / 448.f), nv = __fmul_rn(av, 1.f / 448.f);
-        const float im = am > 0.f ? 1.f / nm : 0.f, iv = av > 0.f ? 1.f / nv : 0.f;
+        const float im = am > 0.f ? __builtin_amdgcn_rcpf(nm) : 0.f, iv = av > 0.f ? __builtin_amdgcn_rcpf(nv) : 0.f;
         float qm[4], qv[4];
+        // (four indices in a row differ in their last two bits: one product for all)
+        const uint32_t row = (((uint32_t)base + 4u * (uint32_t)lane) ^ (t.seed & ~3u)) * kGolden;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t h = noise((uint32_t)(base + place<kVec>(lane, e)), t.seed);
+            const uint32_t h = noise(kVec ? row + ((uint32_t)e ^ (t.seed & 3u)) * kGolden
+                                          : (((uint32_t)base + (uint32_t)place<false>(lane, e)) ^ t.seed) * kGolden);
             qm[e] = round8(__fmul_rn(m[e], im), h & 0xffffu);
             qv[e] = round8(__fmul_rn(rv[e], iv), h >> 16);
             // a second moment that is not zero is not stored as zero: the next
@@ -189,19 +201,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     const Tensor t = a.t[lo];
     Step k{a.b1, a.c1, a.b2, a.c2, a.rate, a.root, a.eps, 1.f, a.grad_scale != nullptr};
     if (k.scaled) k.gs = *a.grad_scale;
-    const int64_t base0 = (int64_t)((int)blockIdx.x - a.start[lo]) * kChunkElems + wave * kPer * kBlockElems;
-    // whole vectors where every array's are aligned
-    constexpr uintptr_t kState = kEight ? 3 : 15;
-    const bool vec = ((uintptr_t)t.p & 15) == 0 && ((uintptr_t)t.g & (4 * sizeof(G) - 1)) == 0 &&
-                     (((uintptr_t)t.m | (uintptr_t)t.v) & kState) == 0 && ((uintptr_t)t.low & 7) == 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int64_t base = base0 + j * kBlockElems;
-        if (base >= t.n) return;
-        const int left = (int)min((int64_t)kBlockElems, t.n - base);
-        if (vec && left == kBlockElems) block<G, kEight, true>(t, k, base, left, lane);
-        else block<G, kEight, false>(t, k, base, left, lane);
-    }
+    const int chunk = (int)blockIdx.x - a.start[lo], first = wave * kBlockElems;
+    const int left = min((chunk == t.chunks - 1 ? t.tail : kChunkElems) - first, kBlockElems);   // elements of this wave
+    if (left <= 0) return;
+    const int64_t base = (int64_t)chunk * kChunkElems + first;
+    if (left == kBlockElems) block<G, kEight, true>(t, k, base, left, lane);
+    else block<G, kEight, false>(t, k, base, left, lane);
 }
 
 }  // namespace

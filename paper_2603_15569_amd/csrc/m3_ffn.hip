@@ -92,10 +92,10 @@ template <typename T, int ROWS, int NW, bool kTurned, bool kPair> struct Tile {
 
 // Bytes that up to `most` of `rows` rows take whose last ends with the 16-byte
 // piece that holds its element cols - 1 (rows are padded to whole pieces).
-template <typename T> __device__ __forceinline__ uint32_t span(int64_t rows, int64_t ld, int64_t cols, int most) {
-    constexpr int64_t EL = 16 / sizeof(T);
-    const int64_t r = min(rows, (int64_t)most);
-    return r <= 0 ? 0u : (uint32_t)(((r - 1) * ld + (cols + EL - 1) / EL * EL) * (int64_t)sizeof(T));
+template <typename T> __device__ __forceinline__ uint32_t span(int rows, int64_t ld, int cols, int most) {
+    constexpr int EL = 16 / (int)sizeof(T);
+    const int r = min(rows, most);
+    return r <= 0 ? 0u : (uint32_t)(r - 1) * (uint32_t)(ld * sizeof(T)) + (uint32_t)((cols + EL - 1) / EL * 16);
 }
 
 // Operand fragments of 16 rows by 64 bytes of k (kk = 0, 1): lane (q, l16) holds
@@ -208,8 +208,8 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
     // A stage's resource: zero past the rows, past k, and after the last step.
     // No branches: the scalar work and the loads go in between the products.
     const uint32_t lda = (uint32_t)(g.lda * sizeof(T)), ldb = (uint32_t)(g.ldb * sizeof(T));
-    const uint32_t sa0 = kAT ? span<T>(1, 0, g.M - m0, 1) : span<T>(g.M - m0, g.lda, g.K, BM);
-    const uint32_t sb0 = kBT ? span<T>(1, 0, g.N - n0, 1) : span<T>(g.N - n0, g.ldb, g.K, NB);
+    const uint32_t sa0 = kAT ? span<T>(1, 0, (int)(g.M - m0), 1) : span<T>((int)(g.M - m0), g.lda, K, BM);
+    const uint32_t sb0 = kBT ? span<T>(1, 0, (int)(g.N - n0), 1) : span<T>((int)(g.N - n0), g.ldb, K, NB);
     auto stage_rsrc = [&](const T *p, bool turned, uint32_t ld, uint32_t span0, int k0, bool in) {
         const int rows = min(K - k0, BK);
         const uint32_t n = turned ? (uint32_t)(rows - 1) * ld + span0 : span0 - (uint32_t)k0 * (uint32_t)sizeof(T);
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
             if (m >= g.M) continue;
             float h[8], dg[8], du[8], dh[8];
             const int64_t at = m * g.ldc + n;
-            const int w = (int)min((int64_t)8, g.ldc - n);   // 8, or 4 in fp32
+            const int w = min(8, (int)(g.ldc - n));   // 8, or 4 in fp32
             if constexpr (KIND == kGateBwd) {
 #pragma unroll
                 for (int p = 0; p < 8; p += 4) {
@@ -443,11 +443,11 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int l16 = lane & 15, q = lane / 16;
     const int64_t r0 = (int64_t)blockIdx.x * RH;
-    const Rsrc rx = make_rsrc(a.x, span<T>(a.T, a.ldx, a.K, kFewRows));
+    const Rsrc rx = make_rsrc(a.x, span<T>((int)a.T, a.ldx, (int)a.K, kFewRows));
     Rsrc rw[NM];
 #pragma unroll
     for (int m = 0; m < NM; ++m)
-        rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>(a.R - r0, a.ldw, a.K, RH));
+        rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>((int)(a.R - r0), a.ldw, (int)a.K, RH));
     const uint32_t wo = (uint32_t)(l16 * (int)(a.ldw * sizeof(T)) + q * 16), wt = (uint32_t)(16 * (int)(a.ldw * sizeof(T)));
     const uint32_t xo = (uint32_t)(l16 * (int)(a.ldx * sizeof(T)) + q * 16), xt = (uint32_t)(16 * (int)(a.ldx * sizeof(T)));
     const int K = (int)a.K, all = (K + U * KS - 1) / (U * KS), split = (int)blockIdx.y;

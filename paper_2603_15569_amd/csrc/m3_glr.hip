@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kFwdWaves * 64, 4) void k_fwd(FwdArgs a) {
     const bool live = d0 < a.D;      // (V divides D)
     const int64_t dl = live ? d0 : 0;
     const int64_t t0 = (int64_t)it.tile * kChunk + wave * S;
-    const int n = (int)max((int64_t)0, min((int64_t)S, a.L - t0));   // tokens of this wave
+    const int n = max(0, min(S, (int)a.L - (int)t0));   // tokens of this wave (L is below 2^31)
 
     const uint32_t lo = live ? (uint32_t)(d0 * sizeof(T)) : kOut;
     const Rows rx = rows<T>(a.x, it.b * a.x_sb + t0 * a.x_st, a.x_st, n, a.D), rr = rows<T>(a.r, it.b * a.r_sb + t0 * a.r_st, a.r_st, n, a.D),
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     const bool live = d0 < a.D;
     const int64_t dl = live ? d0 : 0;
     const int64_t t0 = (int64_t)tile * kChunk + wave * S;
-    const int n = (int)max((int64_t)0, min((int64_t)S, a.L - t0));
+    const int n = max(0, min(S, (int)a.L - (int)t0));
 
     const uint32_t lo = live ? (uint32_t)(d0 * sizeof(T)) : kOut;
     const int64_t orow = (it.b * a.L + t0) * a.D;

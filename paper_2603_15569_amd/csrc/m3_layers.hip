@@ -400,7 +400,8 @@ extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_tens
             if (t.n == 0) continue;
             const int64_t chunks = (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
             if (a.count > 0 && a.start[a.count] + chunks > kMostGroups) break;
-            a.t[a.count] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, t.n, (float)(1.0 - c->lr * t.decay),
+            a.t[a.count] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, (int32_t)chunks,
+                                         (int32_t)(t.n - (chunks - 1) * adamw::kChunkElems), (float)(1.0 - c->lr * t.decay),
                                          (uint32_t)(c->seed + (uint64_t)k)};
             a.start[a.count + 1] = a.start[a.count] + (int32_t)chunks;
             ++a.count;
