@@ -590,8 +590,7 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * AdamW over many tensors (decoupled weight decay), in place, one launch for
- * every 48 tensors, nothing else on the device:
+ * AdamW over many tensors (decoupled weight decay), in place, in one launch:
  *
  *     g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *     p = (1 - lr decay) p - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
@@ -599,8 +598,16 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * p fp32, g fp32 or bf16 (grad_dtype, one for all), m and v fp32, all with n
  * elements; low (NULL: none) receives p rounded to bf16.  grad_scale is a
  * DEVICE scalar (NULL: 1), e.g. the coefficient that clips the gradients'
- * norm.  n = 0 is allowed.  Operations are
- * rounded to fp32 one by one, the root and the quotient within two ulps.
+ * norm.  Operations are rounded to fp32 one by one, the root and the quotient
+ * within two ulps.
+ *
+ * The tensors are described once: m3_adamw_plan_make checks them and fills a
+ * plan and, with host_table not NULL, a table in HOST memory (plan->bytes
+ * bytes, 8-byte aligned; call with NULL first for the size).  The caller copies
+ * the table to the device (16-byte aligned) and passes the plan and the device
+ * copy to every step, as long as the tensors stay where they are.  n = 0 is
+ * allowed.  m3_adamw_step launches nothing but the one kernel and copies
+ * nothing, so it can be captured.
  *
  * 8-bit states (M3_ADAMW_8BIT): m and v hold e4m3 codes (1 byte an element) of
  * m and of sqrt(v), divided by scales[n / 256 rounded up][2] (fp32; m's, then
@@ -608,12 +615,14 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * scale, 0 where all are zero.  Zero codes with any scale are the zero state.
  * They are rounded stochastically with 16 bits each of a hash of the element's
  * index in its tensor and the low 32 bits of (seed + the tensor's place in the
- * call), so pass another seed for every step; a sqrt(v) that is not zero is
+ * list), so pass another seed for every step; a sqrt(v) that is not zero is
  * stored as at least the smallest code.  A non-finite gradient spoils its
  * block.
- * Pointers need their element's alignment only (else M3_ERR_ALIGN).  A NULL table with count > 0, or a NULL pointer in a tensor with n > 0, is
- * M3_ERR_NULL; n < 0, step < 1, a beta outside [0, 1), eps < 0, or a lr,
- * decay or eps that is not finite is M3_ERR_SHAPE.
+ * Pointers need their element's alignment only (else M3_ERR_ALIGN).  A NULL
+ * list with count > 0, or a NULL pointer in a tensor with n > 0, is
+ * M3_ERR_NULL; n < 0, step < 1, a beta outside [0, 1), eps < 0, or a lr, decay
+ * or eps that is not finite is M3_ERR_SHAPE; a table_bytes below the plan's
+ * is M3_ERR_WORKSPACE.
  */
 #define M3_ADAMW_8BIT 1
 typedef struct {
@@ -626,14 +635,20 @@ typedef struct {
     double decay;       /* this tensor's weight decay                        */
 } m3_adamw_tensor;
 typedef struct {
+    int64_t rows, groups;   /* tensors with elements, workgroups of a step   */
+    size_t bytes;           /* of the table                                  */
+    int32_t grad_dtype;     /* m3_dtype of every g                           */
+    int32_t flags;          /* M3_ADAMW_8BIT or 0                            */
+} m3_adamw_plan;
+typedef struct {
     double lr, beta1, beta2, eps;
     int64_t step;       /* t >= 1                                            */
     uint64_t seed;
-    int32_t grad_dtype; /* m3_dtype of every g                               */
-    int32_t flags;      /* M3_ADAMW_8BIT or 0                                */
 } m3_adamw_config;
-m3_status m3_adamw_step(const m3_adamw_config *config, const m3_adamw_tensor *tensors,
-                        int64_t count, const float *grad_scale, void *stream);
+m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t count, int32_t grad_dtype,
+                             int32_t flags, m3_adamw_plan *plan, void *host_table, size_t table_bytes);
+m3_status m3_adamw_step(const m3_adamw_config *config, const m3_adamw_plan *plan,
+                        const void *device_table, const float *grad_scale, void *stream);
 
 /* Static description of a status code. */
 const char *m3_status_string(m3_status status);

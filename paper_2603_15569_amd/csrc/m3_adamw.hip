@@ -1,5 +1,4 @@
-// AdamW over many tensors in one launch (a table of up to kTensors of them
-// goes along as a kernel argument):
+// AdamW over many tensors in one launch, by a table of them on the device:
 //     g' = grad_scale g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2
 //     p = (1 - lr wd) p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 // with m and v in fp32, or in 8 bits: m and sqrt(v) as e4m3 with one fp32
@@ -128,7 +127,7 @@ __device__ __forceinline__ void update(const Step &k, float keep, float g, float
 }
 
 template <typename G, bool kEight, bool kVec>
-__device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t base, int left, int lane) {
+__device__ __forceinline__ void block(const Tensor &t, const Step &k, float keep, uint32_t seed, int64_t base, int left, int lane) {
     float g[4], p[4], m[4], v[4], rv[4];
     load4<G, kVec>(static_cast<const G *>(t.g) + base, lane, left, g);
     load4<float, kVec>(t.p + base, lane, left, p);
@@ -148,7 +147,7 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t ba
         load4<float, kVec>(static_cast<const float *>(t.v) + base, lane, left, v);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) update(k, t.keep, g[e], p[e], m[e], v[e], rv[e]);
+    for (int e = 0; e < 4; ++e) update(k, keep, g[e], p[e], m[e], v[e], rv[e]);
     store4<float, kVec>(t.p + base, lane, left, p);
     if (t.low) store4<bf16, kVec>(static_cast<bf16 *>(t.low) + base, lane, left, p);
     if constexpr (!kEight) {
@@ -173,11 +172,11 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t ba
         const float im = am > 0.f ? __builtin_amdgcn_rcpf(nm) : 0.f, iv = av > 0.f ? __builtin_amdgcn_rcpf(nv) : 0.f;
         float qm[4], qv[4];
         // (four indices in a row differ in their last two bits: one product for all)
-        const uint32_t row = (((uint32_t)base + 4u * (uint32_t)lane) ^ (t.seed & ~3u)) * kGolden;
+        const uint32_t row = (((uint32_t)base + 4u * (uint32_t)lane) ^ (seed & ~3u)) * kGolden;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t h = noise(kVec ? row + ((uint32_t)e ^ (t.seed & 3u)) * kGolden
-                                          : (((uint32_t)base + (uint32_t)place<false>(lane, e)) ^ t.seed) * kGolden);
+            const uint32_t h = noise(kVec ? row + ((uint32_t)e ^ (seed & 3u)) * kGolden
+                                          : (((uint32_t)base + (uint32_t)place<false>(lane, e)) ^ seed) * kGolden);
             qm[e] = round8(__fmul_rn(m[e], im), h & 0xffffu);
             qv[e] = round8(__fmul_rn(rv[e], iv), h >> 16);
             // a second moment that is not zero is not stored as zero: the next
@@ -193,26 +192,23 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, int64_t ba
 template <typename G, bool kEight>
 __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    int lo = 0, hi = a.count - 1;   // the tensor of this workgroup: the last that starts at or before it
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (a.start[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const Tensor t = a.t[lo];
+    const Tensor t = a.t[a.of[blockIdx.x]];
+    const float keep = (float)(1.0 - a.lr * t.decay);
+    const uint32_t seed = a.seed + t.index;
     Step k{a.b1, a.c1, a.b2, a.c2, a.rate, a.root, a.eps, 1.f, a.grad_scale != nullptr};
     if (k.scaled) k.gs = *a.grad_scale;
-    const int chunk = (int)blockIdx.x - a.start[lo], first = wave * kBlockElems;
+    const int chunk = (int)blockIdx.x - t.first, first = wave * kBlockElems;
     const int left = min((chunk == t.chunks - 1 ? t.tail : kChunkElems) - first, kBlockElems);   // elements of this wave
     if (left <= 0) return;
     const int64_t base = (int64_t)chunk * kChunkElems + first;
-    if (left == kBlockElems) block<G, kEight, true>(t, k, base, left, lane);
-    else block<G, kEight, false>(t, k, base, left, lane);
+    if (left == kBlockElems) block<G, kEight, true>(t, k, keep, seed, base, left, lane);
+    else block<G, kEight, false>(t, k, keep, seed, base, left, lane);
 }
 
 }  // namespace
 
 hipError_t launch(const Args &a, bool grad_f32, bool eight, hipStream_t s) {
-    const dim3 grid((unsigned)a.start[a.count]), blk(kWaves * 64);
+    const dim3 grid((unsigned)a.groups), blk(kWaves * 64);
     if (grad_f32 && eight) k_adamw<float, true><<<grid, blk, 0, s>>>(a);
     else if (grad_f32) k_adamw<float, false><<<grid, blk, 0, s>>>(a);
     else if (eight) k_adamw<bf16, true><<<grid, blk, 0, s>>>(a);

@@ -366,49 +366,69 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
 // AdamW
 // ---------------------------------------------------------------------------
 
-extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_tensor *tensors, int64_t count,
-                                   const float *grad_scale, void *stream) {
-    if (!c || (count > 0 && !tensors)) return M3_ERR_NULL;
-    if (c->grad_dtype != M3_F32 && c->grad_dtype != M3_BF16) return M3_ERR_DTYPE;
-    if (count < 0 || c->step < 1 || (c->flags & ~M3_ADAMW_8BIT)) return M3_ERR_SHAPE;
-    if (!std::isfinite(c->lr) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) ||
-        !(c->eps >= 0.0) || !std::isfinite(c->eps))
-        return M3_ERR_SHAPE;
-    const bool eight = (c->flags & M3_ADAMW_8BIT) != 0, gf32 = c->grad_dtype == M3_F32;
-    if (!aligned(grad_scale, 4)) return M3_ERR_ALIGN;
-    for (int64_t k = 0; k < count; ++k) {   // all of them before the first launch
+extern "C" m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t count, int32_t grad_dtype, int32_t flags,
+                                        m3_adamw_plan *plan, void *host_table, size_t table_bytes) {
+    if (!plan || (count > 0 && !tensors)) return M3_ERR_NULL;
+    if (grad_dtype != M3_F32 && grad_dtype != M3_BF16) return M3_ERR_DTYPE;
+    if (count < 0 || count > INT_MAX || (flags & ~M3_ADAMW_8BIT)) return M3_ERR_SHAPE;
+    const bool eight = (flags & M3_ADAMW_8BIT) != 0, gf32 = grad_dtype == M3_F32;
+    int64_t rows = 0, groups = 0;
+    for (int64_t k = 0; k < count; ++k) {
         const m3_adamw_tensor &t = tensors[k];
         if (t.n < 0 || !std::isfinite(t.decay)) return M3_ERR_SHAPE;
-        if (t.n / adamw::kChunkElems >= kMostGroups) return M3_ERR_SHAPE;
         if (t.n == 0) continue;
         if (!t.p || !t.g || !t.m || !t.v || (eight && !t.scales)) return M3_ERR_NULL;
         if (!aligned(t.p, 4) || !aligned(t.g, gf32 ? 4 : 2) || !aligned(t.low, 2) || (eight && !aligned(t.scales, 4)) ||
             (!eight && (!aligned(t.m, 4) || !aligned(t.v, 4))))
             return M3_ERR_ALIGN;
+        if (t.n / adamw::kChunkElems >= 2 * kMostGroups) return M3_ERR_SHAPE;
+        groups += (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
+        if (groups > 2 * kMostGroups) return M3_ERR_SHAPE;
+        ++rows;
     }
+    const size_t head = (size_t)rows * sizeof(adamw::Tensor), bytes = round_up(head + (size_t)groups * sizeof(int32_t), 16);
+    if (host_table) {
+        if (table_bytes < bytes) return M3_ERR_WORKSPACE;
+        if (!aligned(host_table, 8)) return M3_ERR_ALIGN;
+        adamw::Tensor *row = static_cast<adamw::Tensor *>(host_table);
+        int32_t *of = reinterpret_cast<int32_t *>(static_cast<char *>(host_table) + head), first = 0;
+        for (int64_t k = 0, r = 0; k < count; ++k) {
+            const m3_adamw_tensor &t = tensors[k];
+            if (t.n == 0) continue;
+            const int32_t chunks = (int32_t)((t.n + adamw::kChunkElems - 1) / adamw::kChunkElems);
+            row[r] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, first, chunks,
+                                   (int32_t)(t.n - (int64_t)(chunks - 1) * adamw::kChunkElems), (uint32_t)k, t.decay};
+            std::fill(of + first, of + first + chunks, (int32_t)r);
+            first += chunks;
+            ++r;
+        }
+    }
+    *plan = m3_adamw_plan{rows, groups, bytes, grad_dtype, flags};
+    return M3_OK;
+}
+
+extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_plan *plan, const void *table,
+                                   const float *grad_scale, void *stream) {
+    if (!c || !plan || (plan->groups > 0 && !table)) return M3_ERR_NULL;
+    if (plan->grad_dtype != M3_F32 && plan->grad_dtype != M3_BF16) return M3_ERR_DTYPE;
+    if (plan->rows < 0 || plan->rows > plan->groups || plan->groups > 2 * kMostGroups || (plan->flags & ~M3_ADAMW_8BIT) ||
+        c->step < 1)
+        return M3_ERR_SHAPE;
+    if (!std::isfinite(c->lr) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) ||
+        !(c->eps >= 0.0) || !std::isfinite(c->eps))
+        return M3_ERR_SHAPE;
+    if (!aligned(grad_scale, 4) || !aligned(table, 16)) return M3_ERR_ALIGN;
+    if (plan->groups == 0) return M3_OK;
     adamw::Args a;
+    a.t = static_cast<const adamw::Tensor *>(table);
+    a.of = reinterpret_cast<const int32_t *>(a.t + plan->rows);
+    a.groups = (int32_t)plan->groups;
+    a.lr = c->lr;
+    a.seed = (uint32_t)c->seed;
     const double bc1 = 1.0 - std::pow(c->beta1, (double)c->step), bc2 = 1.0 - std::pow(c->beta2, (double)c->step);
     a.b1 = (float)c->beta1; a.c1 = (float)(1.0 - c->beta1);
     a.b2 = (float)c->beta2; a.c2 = (float)(1.0 - c->beta2);
     a.rate = (float)(c->lr / bc1); a.root = (float)std::pow(bc2, -0.5); a.eps = (float)c->eps;
     a.grad_scale = grad_scale;
-    for (int64_t k = 0; k < count;) {
-        a.count = 0;
-        a.start[0] = 0;
-        for (; k < count && a.count < adamw::kTensors; ++k) {
-            const m3_adamw_tensor &t = tensors[k];
-            if (t.n == 0) continue;
-            const int64_t chunks = (t.n + adamw::kChunkElems - 1) / adamw::kChunkElems;
-            if (a.count > 0 && a.start[a.count] + chunks > kMostGroups) break;
-            a.t[a.count] = adamw::Tensor{t.p, t.g, t.m, t.v, t.low, t.scales, (int32_t)chunks,
-                                         (int32_t)(t.n - (chunks - 1) * adamw::kChunkElems), (float)(1.0 - c->lr * t.decay),
-                                         (uint32_t)(c->seed + (uint64_t)k)};
-            a.start[a.count + 1] = a.start[a.count] + (int32_t)chunks;
-            ++a.count;
-        }
-        if (a.count == 0) continue;
-        const m3_status s = launched(adamw::launch(a, gf32, eight, static_cast<hipStream_t>(stream)));
-        if (s != M3_OK) return s;
-    }
-    return M3_OK;
+    return launched(adamw::launch(a, plan->grad_dtype == M3_F32, (plan->flags & M3_ADAMW_8BIT) != 0, static_cast<hipStream_t>(stream)));
 }

@@ -76,7 +76,11 @@ class M3AdamwTensor(ctypes.Structure):
 
 class M3AdamwConfig(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
+
+
+class M3AdamwPlan(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("groups", ctypes.c_int64), ("bytes", ctypes.c_size_t),
                 ("grad_dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
@@ -91,7 +95,7 @@ EXPORTS = ("m3_scan_workspace_bytes", "m3_scan_fwd", "m3_scan_fwd_gated", "m3_sc
            "m3_step", "m3_step_gated", "m3_scan_check", "m3_set_wait_limit", "m3_scan_fwd_noalloc",
            "m3_scan_fwd_pro", "m3_step_pro", "m3_scan_bwd", "m3_scan_bwd_workspace_bytes",
            "m3_glr_workspace_bytes", "m3_glr_fwd", "m3_glr_bwd", "m3_glr_step", "m3_glr_check",
-           "m3_ffn_workspace_bytes", "m3_ffn_fwd", "m3_ffn_bwd", "m3_adamw_step",
+           "m3_ffn_workspace_bytes", "m3_ffn_fwd", "m3_ffn_bwd", "m3_adamw_plan_make", "m3_adamw_step",
            "m3_status_string", "m3_last_hip_error")
 SCRATCH_BYTES = 256 << 20   # M3_SCRATCH_BYTES: the allocation-free scan's fixed workspace
 CTL_BYTES = 1280            # M3_CTL_BYTES: a scan workspace's control block (zero before first use)
@@ -151,9 +155,12 @@ def lib() -> ctypes.CDLL:
         L.m3_ffn_workspace_bytes.restype = ctypes.c_size_t
         L.m3_ffn_fwd.argtypes = [ffn_p] + [vp] * 5 + [vp, ctypes.c_size_t, vp]
         L.m3_ffn_bwd.argtypes = [ffn_p] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
-        L.m3_adamw_step.argtypes = [ctypes.POINTER(M3AdamwConfig), ctypes.POINTER(M3AdamwTensor),
-                                    ctypes.c_int64, vp, vp]
-        for name in ("glr_fwd", "glr_bwd", "glr_step", "glr_check", "ffn_fwd", "ffn_bwd", "adamw_step"):
+        plan_p = ctypes.POINTER(M3AdamwPlan)
+        L.m3_adamw_plan_make.argtypes = [ctypes.POINTER(M3AdamwTensor), ctypes.c_int64, ctypes.c_int32,
+                                         ctypes.c_int32, plan_p, vp, ctypes.c_size_t]
+        L.m3_adamw_step.argtypes = [ctypes.POINTER(M3AdamwConfig), plan_p, vp, vp, vp]
+        for name in ("glr_fwd", "glr_bwd", "glr_step", "glr_check", "ffn_fwd", "ffn_bwd",
+                     "adamw_plan_make", "adamw_step"):
             getattr(L, "m3_" + name).restype = ctypes.c_int
         L.m3_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.m3_set_wait_limit.restype = None
@@ -780,24 +787,25 @@ class AdamWTable:
     """The tensors of an optimizer step as m3_adamw_step takes them (built by
     adamw_table; holds them, so that their memory stays)."""
 
-    def __init__(self, array, grad_dtype, flags, tensors):
-        self.array, self.grad_dtype, self.flags, self.tensors = array, grad_dtype, flags, tensors
+    def __init__(self, plan, table, tensors):
+        self.plan, self.table, self.tensors = plan, table, tensors
 
 
 def adamw_table(params, grads, exp_avg, exp_avg_sq, weight_decay=0.0, low=None, scales=None):
-    """A table of tensors for adamw_step: lists of fp32 params, of grads (fp32 or bf16)
-    and of the states, shaped like the params; `weight_decay` a number or one per
-    tensor; `low` bf16 copies of the params to write.  The states are fp32, or with
-    `scales` (fp32 [ceil(n / 256), 2] each) torch.float8_e4m3fn: e4m3 codes of m and of
-    sqrt(v).  Zeros are the first step's states."""
+    """A table of tensors for adamw_step, built once while they stay where they are:
+    lists of fp32 params, of grads (fp32 or bf16) and of the states, shaped like the
+    params; `weight_decay` a number or one per tensor; `low` bf16 copies of the params
+    to write.  The states are fp32, or with `scales` (fp32 [ceil(n / 256), 2] each)
+    torch.float8_e4m3fn: e4m3 codes of m and of sqrt(v).  Zeros are the first step's
+    states."""
     n = len(params)
     decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
     lists = [grads, exp_avg, exp_avg_sq, decay] + [v for v in (low, scales) if v is not None]
-    if any(len(v) != n for v in lists):
+    if n == 0 or any(len(v) != n for v in lists):
         raise ValueError("adamw_table takes lists of one length")
     eight = scales is not None
     state = torch.float8_e4m3fn if eight else torch.float32
-    gtype = grads[0].dtype if n else torch.float32
+    gtype, dev = grads[0].dtype, params[0].device
     if gtype not in _IO:
         raise ValueError("gradients are fp32 or bf16")
     array = (M3AdamwTensor * n)()
@@ -808,17 +816,22 @@ def adamw_table(params, grads, exp_avg, exp_avg_sq, weight_decay=0.0, low=None, 
         if low is not None:
             want.append(("low", low[k], torch.bfloat16))
         for name, t, dtype in want:
-            if t.dtype != dtype or t.shape != p.shape or t.device != p.device:
-                raise ValueError(f"tensor {k}: {name} must be {dtype} {tuple(p.shape)} on {p.device}")
-        if eight and (scales[k].dtype != torch.float32
+            if t.dtype != dtype or t.shape != p.shape or t.device != dev:
+                raise ValueError(f"tensor {k}: {name} must be {dtype} {tuple(p.shape)} on {dev}")
+        if eight and (scales[k].dtype != torch.float32 or scales[k].device != dev
                       or tuple(scales[k].shape) != (-(-p.numel() // 256), 2)):
             raise ValueError(f"tensor {k}: scales must be fp32 [ceil(n / 256), 2]")
         array[k] = M3AdamwTensor(_p(p), _p(grads[k]), _p(exp_avg[k]), _p(exp_avg_sq[k]),
                                  _p(low[k]) if low is not None else None,
                                  _p(scales[k]) if eight else None, p.numel(), float(decay[k]))
+    plan, make = M3AdamwPlan(), lib().m3_adamw_plan_make
+    args = (array, n, _IO[gtype], M3_ADAMW_8BIT if eight else 0, ctypes.byref(plan))
+    _check(make(*args, None, 0))
+    host = torch.zeros(max(plan.bytes, 16), dtype=torch.uint8)
+    _check(make(*args, host.data_ptr(), host.numel()))
     held = (list(params), list(grads), list(exp_avg), list(exp_avg_sq), low and list(low),
             scales and list(scales))
-    return AdamWTable(array, _IO[gtype], M3_ADAMW_8BIT if eight else 0, held)
+    return AdamWTable(plan, host.to(dev), held)
 
 
 def adamw_step(table: AdamWTable, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -829,6 +842,6 @@ def adamw_step(table: AdamWTable, step: int, lr: float, betas=(0.9, 0.999), eps:
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
         raise ValueError("grad_scale is one fp32 number on the device")
     c = M3AdamwConfig(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step),
-                      int(seed) & (2 ** 64 - 1), table.grad_dtype, table.flags)
-    _check(lib().m3_adamw_step(ctypes.byref(c), table.array, len(table.array),
+                      int(seed) & (2 ** 64 - 1))
+    _check(lib().m3_adamw_step(ctypes.byref(c), ctypes.byref(table.plan), table.table.data_ptr(),
                                None if grad_scale is None else grad_scale.data_ptr(), _stream(stream)))
