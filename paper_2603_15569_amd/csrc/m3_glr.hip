@@ -52,18 +52,23 @@ template <typename T> __device__ __forceinline__ Rows rows(const void *p, int64_
     const int bytes = n > 0 ? (int)((uint32_t)(n - 1) * st + (uint32_t)(width * sizeof(T))) : 0;
     return Rows{__builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(p) + at), (short)0, bytes, 0x00020000), st, n};
 }
+// Outputs go past the caches (kOnce): nothing here reads them again, and the
+// inputs keep the room (4 x 2048 of 4096 forward: 86 us, 77 so).  The
+// backward's loads too, the last use of its inputs (65536 x 2048: 430 us, 409
+// so); the forward's not (82 us), the backward reads them again.
 // (W: the buffer is known to hold the row)
-template <typename R, typename W> __device__ __forceinline__ R row_load(const Rows &w, int s, uint32_t off, W) {
+constexpr int kOnce = 2;
+template <typename R, int kAux = 0, typename W> __device__ __forceinline__ R row_load(const Rows &w, int s, uint32_t off, W) {
     const bool in = W::value || s < w.n;
     const int lane = (int)(in ? off : kOut), row = in ? (int)(s * w.stride) : 0;
-    if constexpr (sizeof(R) == 2) return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b16(w.r, lane, row, 0));
-    else return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b32(w.r, lane, row, 0));
+    if constexpr (sizeof(R) == 2) return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b16(w.r, lane, row, kAux));
+    else return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b32(w.r, lane, row, kAux));
 }
 template <typename R, typename W> __device__ __forceinline__ void row_store(const Rows &w, int s, uint32_t off, R v, W) {
     const bool in = W::value || s < w.n;
     const int lane = (int)(in ? off : kOut), row = in ? (int)(s * w.stride) : 0;
-    if constexpr (sizeof(R) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w.r, lane, row, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w.r, lane, row, 0);
+    if constexpr (sizeof(R) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w.r, lane, row, kOnce);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w.r, lane, row, kOnce);
 }
 // Keeps the compiler from overlapping more tokens than registers are for.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
@@ -408,15 +413,15 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     auto maps = [&](auto whole) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            vr[s] = row_load<R>(rr, s, lo, whole);
-            vi[s] = row_load<R>(ri, s, lo, whole);
-            vx[s] = row_load<R>(rx, s, lo, whole);
-            vd[s] = row_load<R>(rd, s, lo, whole);
+            vr[s] = row_load<R, kOnce>(rr, s, lo, whole);
+            vi[s] = row_load<R, kOnce>(ri, s, lo, whole);
+            vx[s] = row_load<R, kOnce>(rx, s, lo, whole);
+            vd[s] = row_load<R, kOnce>(rd, s, lo, whole);
         }
         if constexpr (kGate) {
             const Rows rz = rows<T>(a.z, it.b * a.z_sb + t0 * a.z_st, a.z_st, n, a.D);
 #pragma unroll
-            for (int s = 0; s < S; ++s) vz[s] = row_load<R>(rz, s, lo, whole);
+            for (int s = 0; s < S; ++s) vz[s] = row_load<R, kOnce>(rz, s, lo, whole);
         }
         fence();
 #pragma unroll
