@@ -14,9 +14,11 @@
 // through them, 6.1 past them).  A wave takes one block of 256 consecutive
 // elements, four a lane, so an 8-bit block's largest magnitude is one wave
 // reduction; more blocks a wave were slower (four: 5.9 TB/s).  Operations are
-// rounded to fp32 one by one; the root and the quotient are the hardware's, an
-// ulp or two off (rounded exactly they made the 8-bit step wait for the vector
-// units: 857 us against KKK for 268 million parameters).
+// rounded to fp32 one by one.  The 8-bit step has enough of them to wait for
+// the vector units: with the library's root and quotients 857 us for 268
+// million parameters (bf16 gradients and copy), 783 (5.5 TB/s) with the
+// hardware's, the ones that the codes depend on refined; without the
+// refinement 717, but an ulp there turns codes over.
 #include "m3_adamw.h"
 #include "m3_device.h"
 
@@ -111,23 +113,38 @@ template <bool kVec> __device__ __forceinline__ void store8(uint8_t *p, int lane
     }
 }
 
+// The root and the reciprocal a rounding step refined: to the nearest but for
+// about one number in a million.  (What the 8-bit codes and scales are formed
+// from: an ulp there can turn a code over, a step of 6% or more.)
+__device__ __forceinline__ float root_near(float v) {
+    const float s = __builtin_amdgcn_rsqf(v), g = v * s;
+    const float r = __fmaf_rn(__fmaf_rn(-g, g, v), 0.5f * s, g);
+    return v > 0x1p-100f && v < __builtin_inff() ? r : __builtin_amdgcn_sqrtf(v);   // (and NaN)
+}
+__device__ __forceinline__ float reciprocal_near(float v) {
+    const float r = __builtin_amdgcn_rcpf(v);
+    return __fmaf_rn(__fmaf_rn(-v, r, 1.f), r, r);
+}
+
 struct Step {
     float b1, c1, b2, c2, rate, root, eps, gs;
     bool scaled;
 };
 
 // One element: m and v, the root of v, and the new p.
-__device__ __forceinline__ void update(const Step &k, float keep, float g, float &p, float &m, float &v, float &rv) {
+template <bool kNear>
+__device__ __forceinline__ void update(const Step &k, float shrink, float g, float &p, float &m, float &v, float &rv) {
 #pragma clang fp contract(off)
     if (k.scaled) g = g * k.gs;
     m = m * k.b1 + g * k.c1;
     v = v * k.b2 + (g * g) * k.c2;
-    rv = __builtin_amdgcn_sqrtf(v);
-    p = p * keep - m * k.rate * __builtin_amdgcn_rcpf(rv * k.root + k.eps);
+    rv = kNear ? root_near(v) : __builtin_amdgcn_sqrtf(v);
+    // (the whole change first: p itself is rounded once)
+    p = p - (p * shrink + m * k.rate * __builtin_amdgcn_rcpf(rv * k.root + k.eps));
 }
 
 template <typename G, bool kEight, bool kVec>
-__device__ __forceinline__ void block(const Tensor &t, const Step &k, float keep, uint32_t seed, int64_t base, int left, int lane) {
+__device__ __forceinline__ void block(const Tensor &t, const Step &k, float shrink, uint32_t seed, int64_t base, int left, int lane) {
     float g[4], p[4], m[4], v[4], rv[4];
     load4<G, kVec>(static_cast<const G *>(t.g) + base, lane, left, g);
     load4<float, kVec>(t.p + base, lane, left, p);
@@ -147,7 +164,7 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, float keep
         load4<float, kVec>(static_cast<const float *>(t.v) + base, lane, left, v);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) update(k, keep, g[e], p[e], m[e], v[e], rv[e]);
+    for (int e = 0; e < 4; ++e) update<kEight>(k, shrink, g[e], p[e], m[e], v[e], rv[e]);
     store4<float, kVec>(t.p + base, lane, left, p);
     if (t.low) store4<bf16, kVec>(static_cast<bf16 *>(t.low) + base, lane, left, p);
     if constexpr (!kEight) {
@@ -169,7 +186,8 @@ __device__ __forceinline__ void block(const Tensor &t, const Step &k, float keep
         if (__any(bad_m)) am = __builtin_nanf("");
         if (__any(bad_v)) av = __builtin_nanf("");
         const float nm = __fmul_rn(am, 1.f / 448.f), nv = __fmul_rn(av, 1.f / 448.f);
-        const float im = am > 0.f ? __builtin_amdgcn_rcpf(nm) : 0.f, iv = av > 0.f ? __builtin_amdgcn_rcpf(nv) : 0.f;
+        // (below 2^-100 a block is stored as zeros; NaN spoils it)
+        const float im = am <= 0x1p-100f ? 0.f : reciprocal_near(nm), iv = av <= 0x1p-100f ? 0.f : reciprocal_near(nv);
         float qm[4], qv[4];
         // (four indices in a row differ in their last two bits: one product for all)
         const uint32_t row = (((uint32_t)base + 4u * (uint32_t)lane) ^ (seed & ~3u)) * kGolden;
@@ -193,7 +211,7 @@ template <typename G, bool kEight>
 __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Tensor t = a.t[a.of[blockIdx.x]];
-    const float keep = (float)(1.0 - a.lr * t.decay);
+    const float shrink = (float)(a.lr * t.decay);
     const uint32_t seed = a.seed + t.index;
     Step k{a.b1, a.c1, a.b2, a.c2, a.rate, a.root, a.eps, 1.f, a.grad_scale != nullptr};
     if (k.scaled) k.gs = *a.grad_scale;
@@ -201,8 +219,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     const int left = min((chunk == t.chunks - 1 ? t.tail : kChunkElems) - first, kBlockElems);   // elements of this wave
     if (left <= 0) return;
     const int64_t base = (int64_t)chunk * kChunkElems + first;
-    if (left == kBlockElems) block<G, kEight, true>(t, k, keep, seed, base, left, lane);
-    else block<G, kEight, false>(t, k, keep, seed, base, left, lane);
+    if (left == kBlockElems) block<G, kEight, true>(t, k, shrink, seed, base, left, lane);
+    else block<G, kEight, false>(t, k, shrink, seed, base, left, lane);
 }
 
 }  // namespace
