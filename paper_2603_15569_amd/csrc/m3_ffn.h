@@ -57,7 +57,7 @@ struct FewArgs {
     int64_t ldo;
     int gelu;
     float *part;           // kPartBytes
-    int splits;            // set at launch
+    int rows, splits;      // set at launch: rows of w a workgroup, parts of k
 };
 hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s);
 

@@ -154,8 +154,17 @@ __device__ __forceinline__ float act(float g, bool gelu, float &slope) {
     return s > 0.f ? f : 0.f * s;
 }
 
+// The waves a SIMD that the compiler schedules for.  Two in bf16, as many as
+// shared memory lets in (8192 x 2048 x 8192 in tiles of 128: 227 us, 276 when it
+// is left to choose).  In fp32 the gates and the products with B alone turned are
+// better left to it (777 tokens, 1000 -> 2730: 71 us a product, 78 with two), the
+// others not (68 us of a weight's gradient, 72).
+template <typename T, bool kAT, bool kBT, Kind KIND> constexpr int waves() {
+    return sizeof(T) == 4 && (KIND != kStore || (kBT && !kAT)) ? 1 : 2;
+}
+
 template <typename T, int BM, int BN, int NWM, int NWN, bool kAT, bool kBT, Kind KIND>
-__global__ __launch_bounds__(NWM * NWN * 64) void k_gemm(GemmArgs g) {
+__global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void k_gemm(GemmArgs g) {
     constexpr int NW = NWM * NWN, BK = kRowBytes / sizeof(T);
     constexpr int WM = BM / NWM, WN = BN / NWN, MT = WM / 16, NT = WN / 16;
     constexpr bool kGates = KIND == kGate || KIND == kGateBwd;
@@ -431,14 +440,16 @@ hipError_t join(const float *part, int64_t ld, int splits, int64_t M, int64_t N,
 // rows of weights (of both gates), its waves interleaved pieces of k, U runs of
 // 64 bytes of every row at a time; the weights are the MFMA's row operand straight from
 // global memory, x (read again by every workgroup, from the caches) its
-// columns, 16 a tile.  The waves' sums meet in LDS.  Without gates k is also
-// split over workgroups (the parts joined after), so that few rows of weights
-// fill the device while a workgroup has enough of them: reading x again costs
-// as many bytes a workgroup as its weights when it has T rows of them.
+// columns, 16 a tile.  The waves' sums meet in LDS.  With RT = 1 it may take
+// half of the MFMA's 16 rows (`rows`, the others' loads being out of range),
+// so that few rows of weights fill the device; without gates k is split over
+// workgroups too (the parts joined after).  Reading x again costs as many bytes
+// a workgroup as its weights when it has T rows of them.
 template <typename T, int TT, int RT, bool kGates>
 __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     constexpr int NW = 8, NM = kGates ? 2 : 1, U = NM * RT * TT >= 8 ? 2 : 4;
-    constexpr int EL = 16 / sizeof(T), KS = 4 * EL, RH = 16 * RT;
+    constexpr int EL = 16 / sizeof(T), KS = 4 * EL;
+    const int RH = RT == 1 ? a.rows : 16 * RT;
     __shared__ f32x4 s_acc[NW][NM * TT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int l16 = lane & 15, q = lane / 16;
@@ -516,7 +527,7 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
                 for (int v = 1; v < NW; ++v) sum[m] += s_acc[v][m * TT + t][ln];
             }
             const int64_t col = t * 16 + ln % 16, r = r0 + 16 * i + ln / 16 * 4;
-            if (col >= a.T || r >= a.Ro) continue;
+            if (col >= a.T || r >= a.Ro || (RT == 1 && ln / 16 * 4 >= RH)) continue;
             if (!kGates && a.splits > 1) {   // (rows of whole fours)
                 const int64_t ld = (a.Ro + 3) / 4 * 4;
                 *reinterpret_cast<f32x4 *>(a.part + ((int64_t)split * a.T + col) * ld + r) = sum[0];
@@ -542,25 +553,30 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     }
 }
 
-template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a, int splits, hipStream_t s) {
+template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a, int rows, int splits, hipStream_t s) {
+    a.rows = rows;
     a.splits = splits;
-    k_few<T, TT, RT, kGates><<<dim3((unsigned)((a.Ro + 16 * RT - 1) / (16 * RT)), (unsigned)splits), dim3(512), 0, s>>>(a);
+    k_few<T, TT, RT, kGates><<<dim3((unsigned)((a.Ro + rows - 1) / rows), (unsigned)splits), dim3(512), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     return join(a.part, (a.Ro + 3) / 4 * 4, splits, a.T, a.Ro, a.out, a.out, 1, a.ldo, sizeof(T) == 4, s);
 }
+// 32 rows a workgroup where there are enough for every compute unit, and where k
+// can be split; 8 where 16 would leave half of the units idle, and k need not be
+// split for them (4096 -> 1024 and back, 8 tokens: 14.7 us, 16.5 with 16 rows
+// of the gates; 8192 -> 2048, one token: 25.3 us a block, 27.1 with 16 rows and
+// four parts, but 30.9 and 30.0 with 16 tokens).
 template <typename T, int TT, bool kGates> hipError_t few(const FewArgs &a, hipStream_t s) {
-    // 32 rows a workgroup where there are enough for every compute unit, and
-    // where k can be split
-    const int64_t wide = (a.Ro + 31) / 32;
+    const int64_t wide = (a.Ro + 31) / 32, groups = (a.Ro + 15) / 16;
     if constexpr (kGates) {
-        return TT > 1 && wide >= 256 ? few_run<T, TT, 2, true>(a, 1, s) : few_run<T, TT, 1, true>(a, 1, s);
+        if (TT > 1 && wide >= 256) return few_run<T, TT, 2, true>(a, 32, 1, s);
+        return few_run<T, TT, 1, true>(a, TT == 1 && groups <= 128 ? 8 : 16, 1, s);
     } else {
-        const int64_t groups = TT > 1 ? wide : (a.Ro + 15) / 16;
+        if (TT == 1 && a.T <= 8 && groups <= 128 && groups >= 64) return few_run<T, TT, 1, false>(a, 8, 1, s);
         // parts of at least 1 KiB of each row for each of the waves
         const int64_t most = std::min<int64_t>(8, a.K * (int64_t)sizeof(T) / 4096);
-        const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / groups));
-        return TT > 1 ? few_run<T, TT, 2, false>(a, splits, s) : few_run<T, TT, 1, false>(a, splits, s);
+        const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / (TT > 1 ? wide : groups)));
+        return TT > 1 ? few_run<T, TT, 2, false>(a, 32, splits, s) : few_run<T, TT, 1, false>(a, 16, splits, s);
     }
 }
 template <typename T, bool kGates> hipError_t few_rows(const FewArgs &a, hipStream_t s) {
@@ -595,15 +611,16 @@ hipError_t run(GemmArgs g, int splits, hipStream_t s) {
 
 // Tile and split of a product, from estimated times (microseconds) fitted to
 // every tile and split of 95 bf16 and 80 fp32 products of the block (100 to
-// 8192 tokens, widths of 512 to 8192); the choice costs 0.8% (bf16) and 0.5%
+// 8192 tokens, widths of 512 to 8192); the choice costs 1.3% (bf16) and 0.7%
 // (fp32) more than the best of them on average.
 //   bf16: a tile of 256 has a compute unit to itself, 128 shares one with
-//     another: rounds of resident workgroups, a step 1.18, and .645 alone to
-//     1.02 shared, 10.3 and 6.2 a round.
+//     another: rounds of resident workgroups, a step 1.18, and .52 alone to
+//     .84 shared, 10.3 and 6.0 a round.
 //   fp32: the matrix units bound either tile, so a unit's workgroups add up:
 //     a step 1.76 (128) or .451 (64) for each of them.
 // Parts cost their bytes, written and read.  (768 x 1024 -> 2816, fp32 gates:
-// 124 us of 128, 84 of 64; 2048 x 8192 -> 2048: 203 and 246 us in bf16.)
+// 125 us of 128, 84 of 64; 8192 -> 2048 of 2048 tokens in bf16: 158 us of 256,
+// 73 of 128.)
 struct Choice {
     bool big;
     int splits;
@@ -624,12 +641,12 @@ template <typename T> Choice choose(const GemmArgs &g, bool gates) {
             double t;
             if (kHalf) {
                 const double rounds = std::ceil(load / (big ? 1 : 2)), share = std::min(std::max(wgs / kUnits - 1.0, 0.0), 1.0);
-                t = rounds * (big ? each * 1.18 + 10.3 : each * (.645 + .38 * share) + 6.2);
+                t = rounds * (big ? each * 1.18 + 10.3 : each * (.52 + .317 * share) + 6.0);
             } else {
                 const double rounds = std::ceil(load / (big ? 2 : 5));
                 t = big ? each * (.15 * rounds + 1.76 * load) + 4.1 * rounds : each * (.106 * rounds + .451 * load) + 2.0 * rounds;
             }
-            if (splits > 1) t += (kHalf ? 1.6 : 2.7) + part * (kHalf ? .45e-6 : .36e-6);
+            if (splits > 1) t += (kHalf ? 1.6 : 2.7) + part * (kHalf ? .48e-6 : .36e-6);
             if (tbest < 0.0 || t < tbest) { tbest = t; best = Choice{big, splits}; }
         }
     }
