@@ -216,6 +216,7 @@ m3_status check_ffn(const m3_ffn_dims *d, bool bwd) {
 struct FfnLayout {
     int64_t Dp, Fp;
     bool pad_d, pad_f;             // weights with rows of dmodel, of dff, are copied
+    int64_t some;                  // tokens the gates' backward takes at a time
     size_t x, dy, wg, wu, wd, h, dg, du, dh, part, total;
 };
 FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
@@ -225,6 +226,10 @@ FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
     w.Fp = (d->dff + el - 1) / el * el;
     w.pad_d = w.Dp != d->dmodel;
     w.pad_f = w.Fp != d->dff;
+    // Tokens whose dh, in tiles of 256, gives each of the 256 compute units one:
+    // up to 64 MB of fp32, read again by the gates while the cache of 256 MB past
+    // L2 has it.
+    w.some = 256 * std::max<int64_t>(1, 256 / ((w.Fp + 255) / 256));
     size_t at = 0;
     auto take = [&](int64_t rows, int64_t cols, int64_t bytes) {
         const size_t here = at;
@@ -239,7 +244,7 @@ FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
     w.h = take(d->tokens, w.Fp, e);
     w.dg = bwd ? take(d->tokens, w.Fp, e) : 0;
     w.du = bwd ? take(d->tokens, w.Fp, e) : 0;
-    w.dh = bwd ? take(d->tokens, w.Fp, 4) : 0;
+    w.dh = bwd ? take(std::min(d->tokens, w.some), w.Fp, 4) : 0;
     w.part = take(1, (int64_t)ffn::kPartBytes, 1);
     w.total = at;
     return w;
@@ -312,9 +317,9 @@ extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd), h{f.ws + w.h, w.Fp};
     if (T <= ffn::kFewRows && f.e == hipSuccess) {
         // (K in whole pieces: the copies are padded with zeros, and so is h)
-        ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU, nullptr, 1};
+        ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU, nullptr, 0, 0};
         f.e = ffn::launch_few(a, f.f32, true, f.stream);
-        a = ffn::FewArgs{h.p, {rd.p, rd.p}, h.ld, rd.ld, T, D, w.Fp, D, y, D, 0, reinterpret_cast<float *>(f.ws + w.part), 1};
+        a = ffn::FewArgs{h.p, {rd.p, rd.p}, h.ld, rd.ld, T, D, w.Fp, D, y, D, 0, reinterpret_cast<float *>(f.ws + w.part), 0, 0};
         if (f.e == hipSuccess) f.e = ffn::launch_few(a, f.f32, false, f.stream);
         return launched(f.e);
     }
@@ -340,16 +345,22 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd);
     const Rows h{f.ws + w.h, w.Fp}, dg{f.ws + w.dg, w.Fp}, du{f.ws + w.du, w.Fp};
-    // dh = dy Wd (with the padding's columns, zero, too)
-    ffn::GemmArgs g = f.args(T, w.Fp, D, ry, rd, f.ws + w.dh, w.Fp);
-    g.f32_out = 1;
-    f.gemm(g, false, true, ffn::kStore);
-    // g and u again; h, dg, du
-    g = f.args(T, F, D, rx, rg, f.ws + w.h, w.Fp);
-    g.b[1] = ru.p;
-    g.dg = f.ws + w.dg; g.du = f.ws + w.du;
-    g.dh = reinterpret_cast<const float *>(f.ws + w.dh);
-    f.gemm(g, false, false, ffn::kGateBwd);
+    const int64_t e = d->io == M3_F32 ? 4 : 2;
+    auto from = [e](Rows r, int64_t t) { return Rows{static_cast<const char *>(r.p) + t * r.ld * e, r.ld}; };
+    ffn::GemmArgs g;
+    for (int64_t t = 0; t < T; t += w.some) {
+        const int64_t n = std::min(w.some, T - t), at = t * w.Fp * e;
+        // dh = dy Wd (with the padding's columns, zero, too)
+        g = f.args(n, w.Fp, D, from(ry, t), rd, f.ws + w.dh, w.Fp);
+        g.f32_out = 1;
+        f.gemm(g, false, true, ffn::kStore);
+        // g and u again; h, dg, du
+        g = f.args(n, F, D, from(rx, t), rg, f.ws + w.h + at, w.Fp);
+        g.b[1] = ru.p;
+        g.dg = f.ws + w.dg + at; g.du = f.ws + w.du + at;
+        g.dh = reinterpret_cast<const float *>(f.ws + w.dh);
+        f.gemm(g, false, false, ffn::kGateBwd);
+    }
     // dx = dg Wg + du Wu
     g = f.args(T, D, F, dg, rg, dx, D);
     g.a[1] = du.p; g.b[1] = ru.p; g.nseg = 2;
