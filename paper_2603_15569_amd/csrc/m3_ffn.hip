@@ -323,21 +323,25 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
         const int64_t n = n0 + wn * 32 + 8 * q;      // (ldc is a multiple of eight, bf16, or four)
         if (n >= g.ldc) return;
         const bool gelu = g.gelu != 0;
+        // (dh's rows are asked for at once, before the first is used: rows past the
+        // last, and columns past a row's four in fp32, as zeros)
+        const int w = min(8, (int)(g.ldc - n));   // 8, or 4 in fp32
+        f32x4 rows[KIND == kGateBwd ? MT : 1][2];
+        if constexpr (KIND == kGateBwd) {
+            const int left = __builtin_amdgcn_readfirstlane(min((int)(g.M - mw), WM)), row = (int)g.ldc * 4;
+            const Rsrc rs = make_rsrc(g.dh + mw * g.ldc, left > 0 ? (uint32_t)(left * row) : 0u);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    rows[i][p] = scan::buf_load<f32x4>(rs, 4 * p < w ? (uint32_t)((16 * i + l16) * row + ((int)n + 4 * p) * 4) : kOut);
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = mw + 16 * i + l16;
             if (m >= g.M) continue;
-            float h[8], dg[8], du[8], dh[8];
+            float h[8], dg[8], du[8];
             const int64_t at = m * g.ldc + n;
-            const int w = min(8, (int)(g.ldc - n));   // 8, or 4 in fp32
-            if constexpr (KIND == kGateBwd) {
-#pragma unroll
-                for (int p = 0; p < 8; p += 4) {
-                    const f32x4 v = p < w ? *reinterpret_cast<const f32x4 *>(g.dh + at + p) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dh[p + e] = v[e];
-                }
-            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float gv = acc[i][e / 4][e % 4], uv = acc[i][2 + e / 4][e % 4];
@@ -345,8 +349,9 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
                 const float f = act(gv, gelu, slope);
                 h[e] = f * uv;
                 if constexpr (KIND == kGateBwd) {
-                    du[e] = dh[e] * f;
-                    dg[e] = dh[e] * uv * slope;
+                    const float dh = rows[i][e / 4][e % 4];
+                    du[e] = dh * f;
+                    dg[e] = dh * uv * slope;
                 }
             }
             auto put = [&](void *dst, const float (&v)[8]) {
