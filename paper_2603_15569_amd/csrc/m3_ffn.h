@@ -12,22 +12,26 @@ namespace ffn {
 // next to each other ([m][k]) or with its own axis so ([k][m], "turned").
 // Rows start on 16 bytes.
 struct GemmArgs {
-    const void *a[2], *b[2];   // two: two products summed (nseg), two products (batch), or the two gates (b)
+    // two: two products summed (nseg), two products (batch), or the two gates (b);
+    // a third product (batch) is N x M, with its own lda, ldb and ldc
+    const void *a[3], *b[3];
     int64_t lda, ldb;          // elements
     int64_t M, N, K;
     int nseg, batch;
-    void *c[2];
+    void *c[3];
     int64_t ldc;
+    int64_t lda3, ldb3, ldc3;
     int f32_out;               // c is fp32 whatever the io dtype
     // gates: h, dg, du with rows of ldc elements (columns N .. ldc - 1 are written as zeros), dh in fp32
     void *dg, *du;
     const float *dh;
     int gelu;
     // set at launch: tiles, and the parts that k is split into (their sums go
-    // to `part`, [product][split][M][part_ld], and are joined there)
+    // to `part`, [product][split], each of part_each elements and in rows of N
+    // rounded up to four, and are joined there)
     int tiles_m, tiles_n, splits;
     float *part;
-    int64_t part_ld;
+    int64_t part_each;
 };
 
 enum Kind {

@@ -176,49 +176,54 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / NWN, wn = wave % NWN, l16 = lane & 15, q = lane / 16;
 
-    // Workgroups go to the XCDs in turn: each XCD gets a run of tiles, eight
-    // rows of tiles at a time, column by column, so that what runs together
-    // on an XCD shares operand rows in its L2.
-    const int total = g.tiles_m * g.tiles_n, id = (int)blockIdx.x;
-    const int xcd = id % 8, per = total / 8, rem = total % 8;
-    const int t = xcd * per + min(xcd, rem) + id / 8;
-    constexpr int GM = 8;
-    const int grp = t / (GM * g.tiles_n), in = t % (GM * g.tiles_n);
-    const int gm = min(GM, g.tiles_m - grp * GM);
     // (divisions leave their results in vector registers: back to scalar ones,
     // where addresses and resources are formed)
     auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    const int64_t m0 = (int64_t)scalar(grp * GM + in % gm) * BM, n0 = (int64_t)scalar(in / gm) * NB;
     const int z = scalar((int)blockIdx.z / g.splits), split = scalar((int)blockIdx.z % g.splits);
+    const bool third = kAT && z == 2;
+    const int64_t M = third ? g.N : g.M, N = third ? g.M : g.N;
+    const int64_t a_ld = third ? g.lda3 : g.lda, b_ld = third ? g.ldb3 : g.ldb, c_ld = third ? g.ldc3 : g.ldc;
+    const int tiles_m = third ? g.tiles_n : g.tiles_m, tiles_n = third ? g.tiles_m : g.tiles_n;
+
+    // Workgroups go to the XCDs in turn: each XCD gets a run of tiles, eight
+    // rows of tiles at a time, column by column, so that what runs together
+    // on an XCD shares operand rows in its L2.
+    const int total = tiles_m * tiles_n, id = (int)blockIdx.x;
+    const int xcd = id % 8, per = total / 8, rem = total % 8;
+    const int t = xcd * per + min(xcd, rem) + id / 8;
+    constexpr int GM = 8;
+    const int grp = t / (GM * tiles_n), in = t % (GM * tiles_n);
+    const int gm = min(GM, tiles_m - grp * GM);
+    const int64_t m0 = (int64_t)scalar(grp * GM + in % gm) * BM, n0 = (int64_t)scalar(in / gm) * NB;
 
     Tile<T, BM, NW, kAT, false> ta;
     Tile<T, BN, NW, kBT, kPair> tb;
-    ta.init(g.lda, wave, lane);
+    ta.init(a_ld, wave, lane);
     if constexpr (kGates) {
         // LDS row r: column r % 32 of wave r / 64's part of Wg (r % 64 < 32) or Wu
 #pragma unroll
         for (int j = 0; j < tb.NI; ++j) {
             const int row = (j * NW + wave) * 8 + lane / 8;
-            tb.off[j] = (uint32_t)((row / 64 * 32 + row % 32) * (int)(g.ldb * sizeof(T)) + ((lane % 8) ^ spread<kPair>(row)) * 16);
+            tb.off[j] = (uint32_t)((row / 64 * 32 + row % 32) * (int)(b_ld * sizeof(T)) + ((lane % 8) ^ spread<kPair>(row)) * 16);
         }
     } else {
-        tb.init(g.ldb, wave, lane);
+        tb.init(b_ld, wave, lane);
     }
 
     const int K = (int)g.K, nk = (K + BK - 1) / BK, steps = nk * g.nseg;
     const int it0 = scalar((int)((int64_t)steps * split / g.splits)), it1 = scalar((int)((int64_t)steps * (split + 1) / g.splits));
     // The tile's operands at k = 0 of the first and of the second product summed
     auto at0 = [](const void *p, bool turned, int64_t ld, int64_t r0) { return static_cast<const T *>(p) + (turned ? r0 : r0 * ld); };
-    const T *pa0 = at0(g.a[kGates ? 0 : z], kAT, g.lda, m0), *pa1 = kGates ? pa0 : at0(g.a[(z + 1) & 1], kAT, g.lda, m0);
-    const T *pb0 = at0(g.b[kGates ? 0 : z], kBT, g.ldb, n0), *pb1 = at0(g.b[kGates ? 1 : (z + 1) & 1], kBT, g.ldb, n0);
+    const T *pa0 = at0(g.a[kGates ? 0 : z], kAT, a_ld, m0), *pa1 = kGates ? pa0 : at0(g.a[(z + 1) & 1], kAT, a_ld, m0);
+    const T *pb0 = at0(g.b[kGates ? 0 : z], kBT, b_ld, n0), *pb1 = at0(g.b[kGates ? 1 : (z + 1) & 1], kBT, b_ld, n0);
     if constexpr (kGates && NW == 8) {   // (a wave's rows are all of Wg, or all of Wu)
         if (wave >= 4) pb0 = pb1;
     }
     // A stage's resource: zero past the rows, past k, and after the last step.
     // No branches: the scalar work and the loads go in between the products.
-    const uint32_t lda = (uint32_t)(g.lda * sizeof(T)), ldb = (uint32_t)(g.ldb * sizeof(T));
-    const uint32_t sa0 = kAT ? span<T>(1, 0, (int)(g.M - m0), 1) : span<T>((int)(g.M - m0), g.lda, K, BM);
-    const uint32_t sb0 = kBT ? span<T>(1, 0, (int)(g.N - n0), 1) : span<T>((int)(g.N - n0), g.ldb, K, NB);
+    const uint32_t lda = (uint32_t)(a_ld * sizeof(T)), ldb = (uint32_t)(b_ld * sizeof(T));
+    const uint32_t sa0 = kAT ? span<T>(1, 0, (int)(M - m0), 1) : span<T>((int)(M - m0), a_ld, K, BM);
+    const uint32_t sb0 = kBT ? span<T>(1, 0, (int)(N - n0), 1) : span<T>((int)(N - n0), b_ld, K, NB);
     auto stage_rsrc = [&](const T *p, bool turned, uint32_t ld, uint32_t span0, int k0, bool in) {
         const int rows = min(K - k0, BK);
         const uint32_t n = turned ? (uint32_t)(rows - 1) * ld + span0 : span0 - (uint32_t)k0 * (uint32_t)sizeof(T);
@@ -321,15 +326,15 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
     const int64_t mw = m0 + wm * WM;
     if constexpr (kGates) {
         const int64_t n = n0 + wn * 32 + 8 * q;      // (ldc is a multiple of eight, bf16, or four)
-        if (n >= g.ldc) return;
+        if (n >= c_ld) return;
         const bool gelu = g.gelu != 0;
         // (dh's rows are asked for at once, before the first is used: rows past the
         // last, and columns past a row's four in fp32, as zeros)
-        const int w = min(8, (int)(g.ldc - n));   // 8, or 4 in fp32
+        const int w = min(8, (int)(c_ld - n));   // 8, or 4 in fp32
         f32x4 rows[KIND == kGateBwd ? MT : 1][2];
         if constexpr (KIND == kGateBwd) {
-            const int left = __builtin_amdgcn_readfirstlane(min((int)(g.M - mw), WM)), row = (int)g.ldc * 4;
-            const Rsrc rs = make_rsrc(g.dh + mw * g.ldc, left > 0 ? (uint32_t)(left * row) : 0u);
+            const int left = __builtin_amdgcn_readfirstlane(min((int)(M - mw), WM)), row = (int)c_ld * 4;
+            const Rsrc rs = make_rsrc(g.dh + mw * c_ld, left > 0 ? (uint32_t)(left * row) : 0u);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -339,9 +344,9 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = mw + 16 * i + l16;
-            if (m >= g.M) continue;
+            if (m >= M) continue;
             float h[8], dg[8], du[8];
-            const int64_t at = m * g.ldc + n;
+            const int64_t at = m * c_ld + n;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float gv = acc[i][e / 4][e % 4], uv = acc[i][2 + e / 4][e % 4];
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int64_t m = mw + 16 * i + l16;
-                if (m >= g.M) continue;
+                if (m >= M) continue;
 #pragma unroll
                 for (int p = 0; p < NT; p += RUN / 4) {
                     const int64_t n = n0 + wn * WN + (kPair ? p / 2 * 32 + 8 * q : 16 * p + 4 * q);
@@ -410,22 +415,32 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
                 }
             }
         };
-        if (g.splits > 1) store(g.part + (int64_t)blockIdx.z * g.M * g.part_ld, g.part_ld, g.part_ld);
-        else if (g.f32_out) store(static_cast<float *>(g.c[z]), g.ldc, g.N);
-        else store(static_cast<T *>(g.c[z]), g.ldc, g.N);
+        const int64_t part_ld = (N + 3) / 4 * 4;
+        if (g.splits > 1) store(g.part + (int64_t)blockIdx.z * g.part_each, part_ld, part_ld);
+        else if (g.f32_out) store(static_cast<float *>(g.c[z]), c_ld, N);
+        else store(static_cast<T *>(g.c[z]), c_ld, N);
     }
 }
 
 // Sums of a product's parts, in order, to the io dtype or fp32: four columns a thread.
-template <typename O> __global__ __launch_bounds__(256) void k_join(const float *part, int64_t ld, int splits, int64_t M, int64_t N,
-                                                                   O *c0, O *c1, int64_t ldc) {
-    const int64_t per = ld / 4, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+struct JoinArgs {
+    const float *part;
+    int64_t each;              // elements of a part
+    int splits;
+    int64_t M, N;              // (a third product is N x M)
+    void *c[3];
+    int64_t ldc, ldc3;
+};
+template <typename O> __global__ __launch_bounds__(256) void k_join(JoinArgs g) {
+    const bool third = blockIdx.y == 2;
+    const int64_t M = third ? g.N : g.M, N = third ? g.M : g.N, ldc = third ? g.ldc3 : g.ldc;
+    const int64_t per = (N + 3) / 4, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (k >= M * per) return;
     const int64_t m = k / per, n = k % per * 4;
-    const float *p = part + ((int64_t)blockIdx.y * splits * M + m) * ld + n;
+    const float *p = g.part + (int64_t)blockIdx.y * g.splits * g.each + m * per * 4 + n;
     f32x4 v = *reinterpret_cast<const f32x4 *>(p);
-    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4 *>(p + s * M * ld);
-    O *o = (blockIdx.y ? c1 : c0) + m * ldc + n;
+    for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4 *>(p + s * g.each);
+    O *o = static_cast<O *>(g.c[blockIdx.y]) + m * ldc + n;
     if (n + 4 <= N && ldc % 4 == 0 && ((uintptr_t)o & (4 * sizeof(O) - 1)) == 0) {
         scan::store4(o, v);
     } else {
@@ -433,11 +448,10 @@ template <typename O> __global__ __launch_bounds__(256) void k_join(const float 
             if (n + e < N) o[e] = (O)v[e];
     }
 }
-hipError_t join(const float *part, int64_t ld, int splits, int64_t M, int64_t N, void *c0, void *c1, int batch, int64_t ldc,
-                bool f32, hipStream_t s) {
-    const dim3 grid((unsigned)((M * (ld / 4) + 255) / 256), (unsigned)batch), block(256);
-    if (f32) k_join<float><<<grid, block, 0, s>>>(part, ld, splits, M, N, static_cast<float *>(c0), static_cast<float *>(c1), ldc);
-    else k_join<bf16><<<grid, block, 0, s>>>(part, ld, splits, M, N, static_cast<bf16 *>(c0), static_cast<bf16 *>(c1), ldc);
+hipError_t join(const JoinArgs &g, int batch, bool f32, hipStream_t s) {
+    const dim3 grid((unsigned)((g.each / 4 + 255) / 256), (unsigned)batch), block(256);
+    if (f32) k_join<float><<<grid, block, 0, s>>>(g);
+    else k_join<bf16><<<grid, block, 0, s>>>(g);
     return hipGetLastError();
 }
 
@@ -564,7 +578,7 @@ template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a,
     k_few<T, TT, RT, kGates><<<dim3((unsigned)((a.Ro + rows - 1) / rows), (unsigned)splits), dim3(512), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    return join(a.part, (a.Ro + 3) / 4 * 4, splits, a.T, a.Ro, a.out, a.out, 1, a.ldo, sizeof(T) == 4, s);
+    return join(JoinArgs{a.part, a.T * ((a.Ro + 3) / 4 * 4), splits, a.T, a.Ro, {a.out}, a.ldo, 0}, 1, sizeof(T) == 4, s);
 }
 // 32 rows a workgroup where there are enough for every compute unit, and where k
 // can be split; 8 where 16 would leave half of the units idle, and k need not be
@@ -593,10 +607,22 @@ template <typename T, bool kGates> hipError_t few_rows(const FewArgs &a, hipStre
     }
 }
 
+// Rows copied to longer ones: 1024 elements a workgroup, each thread's four asked
+// for at once (the sources' rows start on any element).
 template <typename T> __global__ __launch_bounds__(256) void k_pad(const T *src, int64_t src_ld, T *dst, int64_t dst_ld,
                                                                     int64_t cols) {
-    const int64_t row = blockIdx.x;
-    for (int64_t k = threadIdx.x; k < dst_ld; k += 256) dst[row * dst_ld + k] = k < cols ? src[row * src_ld + k] : (T)0.f;
+    const int64_t row = blockIdx.x, k0 = (int64_t)blockIdx.y * 1024 + threadIdx.x;
+    T v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = k0 + 256 * j < cols ? src[row * src_ld + k0 + 256 * j] : (T)0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (k0 + 256 * j < dst_ld) dst[row * dst_ld + k0 + 256 * j] = v[j];
+}
+
+int64_t part_elements(const GemmArgs &g) {
+    const int64_t one = g.M * ((g.N + 3) / 4 * 4), third = g.N * ((g.M + 3) / 4 * 4);
+    return g.batch == 3 ? std::max(one, third) : one;
 }
 
 template <typename T, int BM, int BN, int NWM, int NWN, bool kAT, bool kBT, Kind KIND>
@@ -606,12 +632,13 @@ hipError_t run(GemmArgs g, int splits, hipStream_t s) {
     g.tiles_m = (int)((g.M + BM - 1) / BM);
     g.tiles_n = (int)(((kGates ? g.ldc : g.N) + NB - 1) / NB);
     g.splits = splits;
-    g.part_ld = (g.N + 3) / 4 * 4;
+    g.part_each = part_elements(g);
     k_gemm<T, BM, BN, NWM, NWN, kAT, kBT, KIND>
         <<<dim3((unsigned)(g.tiles_m * g.tiles_n), 1, (unsigned)(g.batch * splits)), dim3(NWM * NWN * 64), 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    return join(g.part, g.part_ld, splits, g.M, g.N, g.c[0], g.c[1], g.batch, g.ldc, sizeof(T) == 4 || g.f32_out, s);
+    return join(JoinArgs{g.part, g.part_each, splits, g.M, g.N, {g.c[0], g.c[1], g.c[2]}, g.ldc, g.ldc3}, g.batch,
+                sizeof(T) == 4 || g.f32_out, s);
 }
 
 // Tile and split of a product, from estimated times (microseconds) fitted to
@@ -640,7 +667,7 @@ template <typename T> Choice choose(const GemmArgs &g, bool gates) {
     for (const bool big : {true, false}) {
         const int64_t b = big ? kBig : kBig / 2, tiles = (g.M + b - 1) / b * ((n + b - 1) / b) * g.batch;
         for (int splits = 1; splits <= (gates ? 1 : 16); ++splits) {
-            const double part = (double)splits * g.batch * g.M * ((g.N + 3) / 4 * 4) * 4.0;
+            const double part = 4.0 * splits * g.batch * part_elements(g);
             if (splits > 1 && (splits > steps || part > (double)kPartBytes)) break;
             const double wgs = (double)tiles * splits, each = std::ceil((double)steps / splits), load = std::ceil(wgs / kUnits);
             double t;
@@ -686,7 +713,7 @@ hipError_t launch_few(const FewArgs &a, bool f32, bool gates, hipStream_t s) {
 }
 hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
                       hipStream_t s) {
-    const dim3 grid((unsigned)rows), block(256);
+    const dim3 grid((unsigned)rows, (unsigned)((dst_ld + 1023) / 1024)), block(256);
     if (f32) k_pad<float><<<grid, block, 0, s>>>(static_cast<const float *>(src), src_ld, static_cast<float *>(dst), dst_ld, cols);
     else k_pad<bf16><<<grid, block, 0, s>>>(static_cast<const bf16 *>(src), src_ld, static_cast<bf16 *>(dst), dst_ld, cols);
     return hipGetLastError();

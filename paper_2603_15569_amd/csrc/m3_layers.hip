@@ -365,11 +365,13 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
     g = f.args(T, D, F, dg, rg, dx, D);
     g.a[1] = du.p; g.b[1] = ru.p; g.nseg = 2;
     f.gemm(g, false, true, ffn::kStore);
-    // dWg = dg^T x, dWu = du^T x
+    // dWg = dg^T x, dWu = du^T x, dWd = dy^T h
     g = f.args(F, D, T, dg, rx, dWg, D);
-    g.a[1] = du.p; g.c[1] = dWu; g.batch = 2;
+    g.a[1] = du.p; g.c[1] = dWu;
+    g.a[2] = ry.p; g.b[2] = h.p; g.c[2] = dWd;
+    g.lda3 = ry.ld; g.ldb3 = h.ld; g.ldc3 = F;
+    g.batch = 3;
     f.gemm(g, true, true, ffn::kStore);
-    f.gemm(f.args(D, F, T, ry, h, dWd, F), true, true, ffn::kStore);
     return launched(f.e);
 }
 
