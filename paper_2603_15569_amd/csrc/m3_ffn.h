@@ -45,9 +45,17 @@ constexpr size_t kPartBytes = (size_t)32 << 20;
 
 // C = A B (both as [row][k], or B or both turned), the two gates
 hipError_t launch_gemm(GemmArgs g, bool f32, bool at, bool bt, Kind kind, hipStream_t s);
-// rows of `cols` elements copied to rows of `ld`, zeros after
-hipError_t launch_pad(const void *src, int64_t src_ld, void *dst, int64_t dst_ld, int64_t rows, int64_t cols, bool f32,
-                      hipStream_t s);
+
+// Rows of `cols` elements copied to rows of dst_ld, zeros after
+struct PadArgs {
+    struct Copy {
+        const void *src;
+        void *dst;
+        int64_t src_ld, dst_ld, rows, cols;
+    } copy[5];
+    int count;
+};
+hipError_t launch_pad(const PadArgs &g, bool f32, hipStream_t s);
 
 // A few rows of x (T of them) times many rows of weights: out[t][r] = sum over
 // k of x(t, k) w(r, k), or the two gates with w[0] = Wg and w[1] = Wu.

@@ -263,13 +263,16 @@ struct Ffn {
     hipStream_t stream;
     bool f32;
     hipError_t e = hipSuccess;
+    ffn::PadArgs pads = {};
 
+    // (copied, where its rows need it, by the launch of copy())
     Rows whole(const void *p, int64_t ld, int64_t rows, int64_t cols, int64_t padded, size_t at) {
         const int64_t es = f32 ? 4 : 2;
         if (padded == cols && ld * es % 16 == 0 && aligned(p, 16)) return Rows{p, ld};
-        if (e == hipSuccess && rows > 0) e = ffn::launch_pad(p, ld, ws + at, padded, rows, cols, f32, stream);
+        if (rows > 0) pads.copy[pads.count++] = {p, ws + at, ld, padded, rows, cols};
         return Rows{ws + at, padded};
     }
+    void copy() { e = ffn::launch_pad(pads, f32, stream); }
     void gemm(const ffn::GemmArgs &g, bool at, bool bt, ffn::Kind kind) {
         if (e == hipSuccess && g.M > 0 && g.N > 0) e = ffn::launch_gemm(g, f32, at, bt, kind, stream);
     }
@@ -315,6 +318,7 @@ extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rx = f.whole(x, d->x_stride, T, D, w.Dp, w.x);
     const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd), h{f.ws + w.h, w.Fp};
+    f.copy();
     if (T <= ffn::kFewRows && f.e == hipSuccess) {
         // (K in whole pieces: the copies are padded with zeros, and so is h)
         ffn::FewArgs a = {rx.p, {rg.p, ru.p}, rx.ld, rg.ld, T, F, w.Dp, w.Fp, f.ws + w.h, w.Fp, d->act == M3_ACT_GELU, nullptr, 0, 0};
@@ -344,6 +348,7 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
     const Rows rx = f.whole(x, d->x_stride, T, D, w.Dp, w.x), ry = f.whole(dy, d->dy_stride, T, D, w.Dp, w.dy);
     const Rows rg = f.whole(Wg, D, F, D, w.Dp, w.wg), ru = f.whole(Wu, D, F, D, w.Dp, w.wu);
     const Rows rd = f.whole(Wd, F, D, F, w.Fp, w.wd);
+    f.copy();
     const Rows h{f.ws + w.h, w.Fp}, dg{f.ws + w.dg, w.Fp}, du{f.ws + w.du, w.Fp};
     const int64_t e = d->io == M3_F32 ? 4 : 2;
     auto from = [e](Rows r, int64_t t) { return Rows{static_cast<const char *>(r.p) + t * r.ld * e, r.ld}; };
