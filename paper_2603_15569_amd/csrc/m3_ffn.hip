@@ -403,7 +403,6 @@ __global__ __launch_bounds__(NWM * NWN * 64, (waves<T, kAT, kBT, KIND>())) void 
         constexpr int RUN = kPair ? 8 : 4;         // columns in a row a lane
         // (c or a part, in fp32 or the io dtype)
         auto store = [&](auto *c, int64_t ldc, int64_t cols) {
-            typedef typename std::remove_pointer<decltype(c)>::type O;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int64_t m = mw + 16 * i + l16;

@@ -574,6 +574,7 @@ __global__ __launch_bounds__(64 * kSumRows) void k_sum(const uint64_t *part, int
     const int64_t d = (int64_t)blockIdx.x * 64 + lane;
     double v = 0.0;
     if (d < D)
+#pragma unroll 8
         for (int64_t k = row; k < rows; k += kSumRows) v += (double)word_value(part[k * D + d]);
     s[row][lane] = v;
     __syncthreads();
