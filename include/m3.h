@@ -1,6 +1,9 @@
 /*
  * libm3 - the Mamba-3 SSM layer's data-parallel hot path on AMD MI355X
- * (gfx950): the chunked prefill scan and the single-token decode step.
+ * (gfx950): the chunked prefill scan and the single-token decode step; and,
+ * at this header's end, what a stack of such layers needs beside them: a gated
+ * linear recurrence (m3_glr_*), the gated feed-forward block (m3_ffn_*), both
+ * with their backward passes, and the AdamW step (m3_adamw_*).
  *
  * The operation (Mamba-3, Sec. 3.1 Prop. "Exponential-Trapezoidal
  * Discretization"; Sec. 3.2 Props. "Complex-to-Real SSM Equivalence" and

@@ -1,4 +1,6 @@
-"""libm3: the Mamba-3 SSM layer's prefill scan and decode step on MI355X.
+"""libm3: the Mamba-3 SSM layer's prefill scan and decode step on MI355X, and
+beside them a gated linear recurrence, the gated feed-forward block (both with
+their backward passes) and the AdamW step.
 
 The compute path is the HIP library libm3.so (C ABI in include/m3.h); this
 package holds its sources (csrc/), the build script, the ctypes binding (m3)

@@ -13,7 +13,8 @@
 // nothing of it that is used again: 268 million parameters in fp32, 5.5 TB/s
 // through them, 6.1 past them).  A wave takes one block of 256 consecutive
 // elements, four a lane, so an 8-bit block's largest magnitude is one wave
-// reduction; more blocks a wave were slower (four: 5.9 TB/s).  Operations are
+// reduction; more blocks a wave were slower (four: 5.9 TB/s).  132 small tensors
+// of 2.4 million elements in all: 13.5 us, 11 of them the bytes'.  Operations are
 // rounded to fp32 one by one.  The 8-bit step has enough of them to wait for
 // the vector units: with the library's root and quotients 857 us for 268
 // million parameters (bf16 gradients and copy), 783 (5.5 TB/s) with the

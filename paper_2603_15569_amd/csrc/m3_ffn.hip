@@ -9,6 +9,19 @@
 // holds g and u of the same elements.  Operands whose k runs down the rows
 // (the gradients') are read out of LDS with the transposing read.
 //
+// Tiles: 256 x 256 in bf16 (eight waves of 128 x 64, a compute unit to itself)
+// where there are enough of them, 128 x 128 (four of 64 x 64, two workgroups a
+// unit) elsewhere; 128 and 64 in fp32.  The larger a wave's tile, the fewer bytes
+// of LDS a product: a step of the large one reads 192 KB and writes 64 KB for
+// 2048 cycles of the matrix units.  8192 tokens, 2048 -> 8192 in bf16: the gates
+// 401 us (1370 TFLOP/s), the way back 192 (1430), where a library's product of
+// this size reaches 1610; with everything on the card at work a step takes 1.54
+// us, with 32 units 1.1, so the clock and the operands' way through L2 bound it,
+// and next the epilogues, which nothing else hides (5 us a round of tiles, 22
+// in the backward, whose gates read dh and write three arrays).  fp32: the matrix
+// units, 140 TFLOP/s of the library's 154 (2048 tokens, 2048 -> 8192); small
+// products lose a third of it to the last round of tiles.
+//
 // Edges: buffer loads return zero past the end of an operand, so rows past M,
 // N or (turned) K need no masks; k past K within a row is sent out of range.
 #include <algorithm>
@@ -460,7 +473,10 @@ hipError_t join(const JoinArgs &g, int batch, bool f32, hipStream_t s) {
 // half of the MFMA's 16 rows (`rows`, the others' loads being out of range),
 // so that few rows of weights fill the device; without gates k is split over
 // workgroups too (the parts joined after).  Reading x again costs as many bytes
-// a workgroup as its weights when it has T rows of them.
+// a workgroup as its weights when it has T rows of them.  2048 -> 8192 in bf16:
+// one token 13.4 us the gates (5.0 TB/s of weights), 8.9 the way back (3.8); 48
+// tokens 18.6 and 13.3: the launch, the first loads' latency and the meeting in
+// LDS are what is left.
 template <typename T, int TT, int RT, bool kGates>
 __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     constexpr int NW = 8, NM = kGates ? 2 : 1, U = NM * RT * TT >= 8 ? 2 : 4;

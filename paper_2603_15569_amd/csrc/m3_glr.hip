@@ -14,6 +14,13 @@
 // wait in registers meanwhile.  The backward runs the same way from the last
 // tile to the first on q_t = a_t (dh_t + q_{t+1}), with the states entering
 // the tiles as the forward saved them.
+//
+// Bound by HBM, and by the look-back where a sequence has few tiles: 16 tokens a
+// wave are what its registers hold with the gate (123 of them), so a compute unit
+// keeps 200 KB of loads on their way.  65536 tokens of 2048 channels in bf16:
+// forward 250 us (4.3 TB/s), backward 405 (4.6); 4 x 2048 of 4096 with the gate
+// and inputs as slices: 75 us (4.5).  3 x 1001 tokens of 1000 channels in fp32, one
+// and a half workgroups a unit: 18 us forward, 32 backward.
 #include <type_traits>
 
 #include "m3_device.h"
@@ -164,8 +171,8 @@ struct Words {
 // there (32 tiles of 512 channels: 13.9 us against 19.7 without; further into
 // a sequence the wider polling costs more than it saves, 261 us -> 284 at 512
 // tiles of 2048 channels).  The nearest tile whose state is known, with the
-// maps of all after it, gives the state, folded in token order.  `enter` is the state of the lane's channels,
-// NaN when the wait gave up.
+// maps of all after it, gives the state, folded in token order.  `enter` is the
+// state of the lane's channels, NaN when the wait gave up.
 constexpr int kReach = 4;
 template <int V, int NW> struct Polled {
     float v[kReach * NW][2][64 * V];   // the state after the tile, or its map
@@ -566,7 +573,8 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     }
 }
 
-// dA: the tiles' parts of a channel summed in fp64, in one order.
+// dA: the tiles' parts of a channel summed in fp64, in one order (512 of 2048
+// channels: 6.7 us with eight of a thread's loads at once, 11 one by one).
 constexpr int kSumRows = 16;
 __global__ __launch_bounds__(64 * kSumRows) void k_sum(const uint64_t *part, int64_t rows, int64_t D, float *dA) {
     __shared__ double s[kSumRows][64];
@@ -591,7 +599,8 @@ __global__ __launch_bounds__(256) void k_empty(const float *in, float *out, int6
     if (dA && k < D) dA[k] = 0.f;
 }
 
-// One token: the state is read and written once.
+// One token: the state is read and written once (64 rows of 4096 channels with
+// the gate: 4.7 MB, 2.8 us, a launch's own time).
 template <typename T, int V, bool kGate>
 __global__ __launch_bounds__(256) void k_step(StepArgs a) {
     typedef typename Raw<T, V>::type R;
