@@ -569,32 +569,48 @@ def scan_bwd(x, Bm, Cm, dt, A, lam, theta, D, dy, chunk: int, dfinal=None, init_
 # ---------------------------------------------------------------------------
 
 def _meta(t: Optional[torch.Tensor]):
-    """What the checks of a tensor go by."""
-    return None if t is None else (t.shape, t.dtype, t.device, t.stride())
+    """What the checks of a tensor go by (a call's checks are kept by it: a program
+    makes the same ones again and again)."""
+    return None if t is None else (t.shape, t.dtype, t.get_device(), t.stride())
 
 
 def _empty(t: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
-def _f32(t: Optional[torch.Tensor], shape, dev, name: str):
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _dense(name: str, t, shape, dtype, dev) -> None:
+    """Raises unless the tensor of meta `t` (None: there is none) is contiguous, of
+    this shape, type and device."""
     if t is None:
-        return None
-    if t.shape != shape or t.dtype is not torch.float32 or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous fp32 {tuple(shape)} on {dev}")
-    return t.data_ptr()
+        return
+    step, dense = 1, True
+    for n, st in zip(reversed(t[0]), reversed(t[3])):
+        dense = dense and (n == 1 or st == step)
+        step *= n
+    if tuple(t[0]) != tuple(shape) or t[1] is not dtype or t[2] != dev or not (dense or step == 0):
+        raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on the device of x")
 
 
-def _like(t: torch.Tensor, shape, dtype, dev, name: str):
-    if t.shape != shape or t.dtype is not dtype or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {dev}")
-    return t.data_ptr()
+def _on_gpu(x) -> None:
+    if x[2] < 0:
+        raise ValueError("libm3 takes tensors of a GPU")
+
+
+def _work(t: torch.Tensor, x: torch.Tensor):
+    """A workspace's address and bytes."""
+    if t.dtype is not torch.uint8 or t.get_device() != x.get_device() or not t.is_contiguous():
+        raise ValueError("a workspace is contiguous bytes (torch.uint8) on the device of x")
+    return t.data_ptr(), t.numel()
 
 
 @functools.lru_cache(maxsize=256)
 def _glr_dims(x, r, i, z) -> M3GlrDims:
-    """The dims of a recurrence by the tensors' shapes, types and strides, checked (a
-    program makes the same ones again and again; the library only reads them)."""
+    """The dims of a recurrence by the tensors' metas, checked (the library only reads
+    them)."""
     shape, dtype = x[0], x[1]
     if dtype not in _IO:
         raise ValueError("x must be fp32 or bf16")
@@ -613,6 +629,20 @@ def _glr_dims(x, r, i, z) -> M3GlrDims:
         st = [t[3][k] if shape[k] > 1 else 0 for k in range(len(shape) - 1)]
         strides += [st[0], st[1] if len(st) > 1 else 0]
     return M3GlrDims(shape[0], 1 if len(shape) == 2 else shape[1], shape[-1], _IO[dtype], 0, *strides)
+
+
+@functools.lru_cache(maxsize=256)
+def _glr_call(x, r, i, z, A, like, states, *state) -> M3GlrDims:
+    """The dims of a call on x [B, L, D] (a step: [B, D]), and the checks of its other
+    tensors: A [D], one like x, the saved states, and states [B, D]."""
+    d, dev = _glr_dims(x, r, i, z), x[2]
+    _dense("A", A, (d.width,), torch.float32, dev)
+    _dense("y or dy", like, x[0], x[1], dev)
+    _dense("states", states, (d.batch, -(-d.seqlen // GLR_CHUNK), d.width), torch.float32, dev)
+    for t in state:
+        _dense("a state or its gradient", t, (d.batch, d.width), torch.float32, dev)
+    _on_gpu(x)
+    return d
 
 
 def glr_dims(x, r=None, i=None, z=None) -> M3GlrDims:
@@ -644,22 +674,17 @@ def glr_fwd(x, r, i, A, z=None, init_state=None, save_states: bool = False, out=
     fp32, channels next to each other, any batch and token strides), A [D] fp32.
     Returns y [B, L, D], final_state [B, D] fp32 and, with `save_states`, the states
     that glr_bwd takes.  `out` may supply (y, final_state)."""
-    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
-    shape, dtype, dev = x.shape, x.dtype, x.device
-    B, L, D = shape
+    y, fs = (None, None) if out is None else out
+    B, L, D = x.shape
+    d = _glr_call(_meta(x), _meta(r), _meta(i), _meta(z), _meta(A), _meta(y), None, _meta(init_state), _meta(fs))
     if out is None:
-        y = _empty(x)
-        fs = torch.empty((B, D), dtype=torch.float32, device=dev)
-    else:
-        y, fs = out
-    states = torch.empty((B, -(-L // GLR_CHUNK), D), dtype=torch.float32, device=dev) if save_states else None
+        y, fs = _empty(x), A.new_empty((B, D))
+    states = A.new_empty((B, -(-L // GLR_CHUNK), D)) if save_states else None
     if workspace is None:
         workspace = glr_workspace(x, r, i, z)
-    _check(lib().m3_glr_fwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
-                            _f32(A, (D,), dev, "A"), None if z is None else z.data_ptr(),
-                            _f32(init_state, (B, D), dev, "init_state"),
-                            _like(y, shape, dtype, dev, "y"), _f32(fs, (B, D), dev, "final_state"),
-                            _p(states), _p(workspace), workspace.numel(), _stream(stream)))
+    _check(lib().m3_glr_fwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(), A.data_ptr(), _ptr(z),
+                            _ptr(init_state), y.data_ptr(), fs.data_ptr(), _ptr(states), *_work(workspace, x),
+                            _stream(stream)))
     return (y, fs, states) if save_states else (y, fs)
 
 
@@ -668,40 +693,35 @@ def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = Fals
     """m3_glr_bwd: gradients of J = <dy, y> + <dfinal, final_state>, from the forward's
     inputs and the states it saved.  Returns a dict: dx, dr, di (dz) in the io dtype,
     dA [D] fp32 and, with `want_dinit`, dinit [B, D] fp32."""
-    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
-    shape, dtype, dev = x.shape, x.dtype, x.device
-    B, L, D = shape
+    B, _, D = x.shape
+    if states is None or dy is None:
+        raise ValueError("glr_bwd takes the forward's states and dy")
+    d = _glr_call(_meta(x), _meta(r), _meta(i), _meta(z), _meta(A), _meta(dy), _meta(states), _meta(dfinal))
     out = {k: _empty(x)
            for k in (("dx", "dr", "di") if z is None else ("dx", "dr", "di", "dz"))}
-    out["dA"] = torch.empty((D,), dtype=torch.float32, device=dev)
+    out["dA"] = A.new_empty((D,))
     if want_dinit:
-        out["dinit"] = torch.empty((B, D), dtype=torch.float32, device=dev)
+        out["dinit"] = A.new_empty((B, D))
     if workspace is None:
         workspace = glr_workspace(x, r, i, z)
-    _check(lib().m3_glr_bwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(),
-                            _f32(A, (D,), dev, "A"), None if z is None else z.data_ptr(),
-                            _f32(states, (B, -(-L // GLR_CHUNK), D), dev, "states"),
-                            _like(dy, shape, dtype, dev, "dy"), _f32(dfinal, (B, D), dev, "dfinal"),
-                            out["dx"].data_ptr(), out["dr"].data_ptr(), out["di"].data_ptr(),
-                            None if z is None else out["dz"].data_ptr(), out["dA"].data_ptr(),
-                            out["dinit"].data_ptr() if want_dinit else None,
-                            _p(workspace), workspace.numel(), _stream(stream)))
+    _check(lib().m3_glr_bwd(ctypes.byref(d), x.data_ptr(), r.data_ptr(), i.data_ptr(), A.data_ptr(), _ptr(z),
+                            states.data_ptr(), dy.data_ptr(), _ptr(dfinal), out["dx"].data_ptr(),
+                            out["dr"].data_ptr(), out["di"].data_ptr(), _ptr(out.get("dz")),
+                            out["dA"].data_ptr(), _ptr(out.get("dinit")), *_work(workspace, x),
+                            _stream(stream)))
     return out
 
 
 def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
     """m3_glr_step: one token, x, r, i, z [B, D]; advances `state` [B, D] fp32 in
     place and returns y [B, D]."""
-    d = _glr_dims(_meta(x), _meta(r), _meta(i), _meta(z))
-    shape, dtype, dev = x.shape, x.dtype, x.device
-    if len(shape) != 2:
-        raise ValueError(f"x must be [B, D], got {tuple(shape)}")
+    if x.dim() != 2:
+        raise ValueError(f"x must be [B, D], got {tuple(x.shape)}")
+    d = _glr_call(_meta(x), _meta(r), _meta(i), _meta(z), _meta(A), _meta(y), None, _meta(state))
     if y is None:
         y = _empty(x)
-    _check(lib().m3_glr_step(ctypes.byref(d), _f32(state, shape, dev, "state"), x.data_ptr(),
-                             r.data_ptr(), i.data_ptr(), _f32(A, shape[1:], dev, "A"),
-                             None if z is None else z.data_ptr(), _like(y, shape, dtype, dev, "y"),
-                             _stream(stream)))
+    _check(lib().m3_glr_step(ctypes.byref(d), state.data_ptr(), x.data_ptr(), r.data_ptr(), i.data_ptr(),
+                             A.data_ptr(), _ptr(z), y.data_ptr(), _stream(stream)))
     return y
 
 
@@ -710,17 +730,17 @@ def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
 # ---------------------------------------------------------------------------
 
 @functools.lru_cache(maxsize=256)
-def _ffn_dims(x, Wg, Wu, Wd, dy, act) -> M3FfnDims:
-    """The dims of a block by the tensors' shapes, types and strides, checked."""
-    shape, dtype, dev, strides = x
+def _ffn_dims(x, Wg, Wu, Wd, y, dy, act) -> M3FfnDims:
+    """The dims of a block by the tensors' metas, checked."""
+    shape, dtype, dev = x[:3]
     if dtype not in _IO:
         raise ValueError("x must be fp32 or bf16")
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}")
     D, F = shape[-1], Wg[0][0]
     for name, t, want in (("Wg", Wg, (F, D)), ("Wu", Wu, (F, D)), ("Wd", Wd, (D, F))):
-        if t is not None and (t[0] != want or t[1] != dtype or t[2] != dev):
-            raise ValueError(f"{name} must be {dtype} {want} on {dev}")
+        _dense(name, t, want, dtype, dev)
+    _dense("y", y, shape, dtype, dev)
     rows = []
     for name, t in (("x", x), ("dy", dy)):
         if t is None:
@@ -740,13 +760,14 @@ def _ffn_dims(x, Wg, Wu, Wd, dy, act) -> M3FfnDims:
     T = 1
     for n in shape[:-1]:
         T *= n
+    _on_gpu(x)
     return M3FfnDims(T, D, F, _IO[dtype], _ACT[act], *rows)
 
 
 def ffn_workspace(x, Wg, backward: bool = False) -> torch.Tensor:
     """A workspace for ffn_fwd (ffn_bwd with `backward`, which serves both) of x
     [..., D] and Wg [F, D]: keep it for further calls, one at a time."""
-    d = _ffn_dims(_meta(x), _meta(Wg), None, None, None, "silu")
+    d = _ffn_dims(_meta(x), _meta(Wg), None, None, None, None, "silu")
     n = int(lib().m3_ffn_workspace_bytes(ctypes.byref(d), int(backward)))
     return torch.empty(max(n, 16), dtype=torch.uint8, device=x.device)
 
@@ -755,27 +776,25 @@ def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=N
     """m3_ffn_fwd: y = (act(x Wg^T) o (x Wu^T)) Wd^T; x [..., D] (rows at one stride), Wg
     and Wu [F, D], Wd [D, F], bf16 or fp32; act "silu" or "gelu" (tanh form).  Returns
     y, shaped like x, contiguous."""
-    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), None, act)
-    shape, dtype, dev = x.shape, x.dtype, x.device
+    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), _meta(out), None, act)
     y = out if out is not None else _empty(x)
     if workspace is None:
         workspace = ffn_workspace(x, Wg)
-    _check(lib().m3_ffn_fwd(ctypes.byref(d), x.data_ptr(), _p(Wg), _p(Wu), _p(Wd),
-                            _like(y, shape, dtype, dev, "y"), _p(workspace), workspace.numel(),
-                            _stream(stream)))
+    _check(lib().m3_ffn_fwd(ctypes.byref(d), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
+                            y.data_ptr(), *_work(workspace, x), _stream(stream)))
     return y
 
 
 def ffn_bwd(x, Wg, Wu, Wd, dy, act: str = "silu", workspace=None, stream=None):
     """m3_ffn_bwd: gradients of J = <dy, y> from the forward's inputs (g and u are formed
     again).  Returns a dict: dx (shaped like x), dWg, dWu, dWd, in the io dtype."""
-    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), _meta(dy), act)
+    d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), None, _meta(dy), act)
     out = dict(dx=_empty(x), dWg=_empty(Wg), dWu=_empty(Wu), dWd=_empty(Wd))
     if workspace is None:
         workspace = ffn_workspace(x, Wg, backward=True)
-    _check(lib().m3_ffn_bwd(ctypes.byref(d), x.data_ptr(), _p(Wg), _p(Wu), _p(Wd), dy.data_ptr(),
-                            _p(out["dx"]), _p(out["dWg"]), _p(out["dWu"]), _p(out["dWd"]), _p(workspace),
-                            workspace.numel(), _stream(stream)))
+    _check(lib().m3_ffn_bwd(ctypes.byref(d), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
+                            dy.data_ptr(), out["dx"].data_ptr(), out["dWg"].data_ptr(), out["dWu"].data_ptr(),
+                            out["dWd"].data_ptr(), *_work(workspace, x), _stream(stream)))
     return out
 
 
@@ -839,8 +858,11 @@ def adamw_step(table: AdamWTable, step: int, lr: float, betas=(0.9, 0.999), eps:
     """m3_adamw_step: one AdamW step (the `step`-th, from 1) over the table's tensors, in
     place.  `grad_scale` is a device scalar that every gradient is multiplied by (None:
     1); `seed` feeds the 8-bit states' stochastic rounding: another for every step."""
-    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
+                                   or grad_scale.get_device() != table.table.get_device()):
         raise ValueError("grad_scale is one fp32 number on the device")
+    if table.table.get_device() < 0:
+        raise ValueError("libm3 takes tensors of a GPU")
     c = M3AdamwConfig(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step),
                       int(seed) & (2 ** 64 - 1))
     _check(lib().m3_adamw_step(ctypes.byref(c), ctypes.byref(table.plan), table.table.data_ptr(),

@@ -236,3 +236,34 @@ def test_binding_refusals():
         m3.adamw_table(p, p, p, p, scales=[torch.zeros(1, 2)] * 2)       # states not in 8 bits
     with pytest.raises(ValueError):
         m3.adamw_step(m3.adamw_table(p, p, p, p), step=1, lr=1.0, grad_scale=torch.zeros(2))
+
+
+def test_binding_refuses_host_tensors():
+    """Calls that are right but for lying in host memory."""
+    x, A = torch.zeros(2, 5, 8, dtype=torch.bfloat16), -torch.ones(8)
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    W, Wd = torch.zeros(12, 8, dtype=torch.bfloat16), torch.zeros(8, 12, dtype=torch.bfloat16)
+    p, s = [torch.zeros(4)], torch.zeros(2, 1, 8)
+    for call in (lambda: m3.glr_fwd(x, x, x, A, workspace=ws), lambda: m3.glr_bwd(x, x, x, A, s, x, workspace=ws),
+                 lambda: m3.glr_step(torch.zeros(2, 8), x[:, 0], x[:, 0], x[:, 0], A),
+                 lambda: m3.ffn_fwd(x, W, W, Wd, workspace=ws), lambda: m3.ffn_bwd(x, W, W, Wd, x, workspace=ws),
+                 lambda: m3.adamw_step(m3.adamw_table(p, p, p, p), step=1, lr=1.0)):
+        with pytest.raises(ValueError, match="of a GPU"):
+            call()
+
+
+@pytest.mark.gpu
+def test_binding_refuses_workspaces_and_scalars_elsewhere():
+    x, A = torch.zeros(2, 5, 8, dtype=torch.bfloat16, device="cuda"), -torch.ones(8, device="cuda")
+    W, Wd = x.new_zeros(12, 8), x.new_zeros(8, 12)
+    for ws in (torch.zeros(1 << 26, dtype=torch.uint8), torch.zeros(1 << 24, device="cuda"),
+               torch.zeros(1 << 27, dtype=torch.uint8, device="cuda")[::2]):
+        for call in (lambda: m3.glr_fwd(x, x, x, A, workspace=ws), lambda: m3.ffn_fwd(x, W, W, Wd, workspace=ws),
+                     lambda: m3.ffn_bwd(x, W, W, Wd, x, workspace=ws)):
+            with pytest.raises(ValueError, match="workspace"):
+                call()
+    with pytest.raises(ValueError):
+        m3.glr_fwd(x, x, x, A.cpu())
+    p = [torch.zeros(4, device="cuda")]
+    with pytest.raises(ValueError):
+        m3.adamw_step(m3.adamw_table(p, p, p, p), step=1, lr=1.0, grad_scale=torch.ones(1))
