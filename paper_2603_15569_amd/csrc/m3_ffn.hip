@@ -465,32 +465,28 @@ hipError_t join(const JoinArgs &g, int batch, bool f32, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Few rows of x: bound by reading the weights once.  A workgroup takes 16 RT
+// Few rows of x: bound by reading the weights once.  A workgroup takes up to 16 RT
 // rows of weights (of both gates), its waves interleaved pieces of k, U runs of
 // 64 bytes of every row at a time; the weights are the MFMA's row operand straight from
-// global memory, x (read again by every workgroup, from the caches) its
-// columns, 16 a tile.  The waves' sums meet in LDS.  With RT = 1 it may take
-// half of the MFMA's 16 rows (`rows`, the others' loads being out of range),
-// so that few rows of weights fill the device; without gates k is split over
-// workgroups too (the parts joined after).  Reading x again costs as many bytes
-// a workgroup as its weights when it has T rows of them.  2048 -> 8192 in bf16:
-// one token 13.4 us the gates (5.0 TB/s of weights), 8.9 the way back (3.8); 48
-// tokens 18.6 and 13.3: the launch, the first loads' latency and the meeting in
-// LDS are what is left.
+// global memory (rows past the workgroup's out of range), x (read again by every
+// workgroup, from the caches) its columns, 16 a tile.  The waves' sums meet in LDS.
+// Without gates k may be split over workgroups too (the parts joined after).
+// Loading x a unit ahead as well cost more in registers than it gave (48 tokens:
+// 39.5 us a block, 41.8).  2048 -> 8192 in bf16: one token 12.5 us the gates (5.4
+// TB/s of weights), 9.0 the way back (3.7); 48 tokens 18 and 13.5.
 template <typename T, int TT, int RT, bool kGates>
 __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     constexpr int NW = 8, NM = kGates ? 2 : 1, U = NM * RT * TT >= 8 ? 2 : 4;
     constexpr int EL = 16 / sizeof(T), KS = 4 * EL;
-    const int RH = RT == 1 ? a.rows : 16 * RT;
     __shared__ f32x4 s_acc[NW][NM * TT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int l16 = lane & 15, q = lane / 16;
-    const int64_t r0 = (int64_t)blockIdx.x * RH;
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows;
     const Rsrc rx = make_rsrc(a.x, span<T>((int)a.T, a.ldx, (int)a.K, kFewRows));
     Rsrc rw[NM];
 #pragma unroll
     for (int m = 0; m < NM; ++m)
-        rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>((int)(a.R - r0), a.ldw, (int)a.K, RH));
+        rw[m] = make_rsrc(static_cast<const T *>(a.w[m]) + r0 * a.ldw, span<T>((int)(a.R - r0), a.ldw, (int)a.K, a.rows));
     const uint32_t wo = (uint32_t)(l16 * (int)(a.ldw * sizeof(T)) + q * 16), wt = (uint32_t)(16 * (int)(a.ldw * sizeof(T)));
     const uint32_t xo = (uint32_t)(l16 * (int)(a.ldx * sizeof(T)) + q * 16), xt = (uint32_t)(16 * (int)(a.ldx * sizeof(T)));
     const int K = (int)a.K, all = (K + U * KS - 1) / (U * KS), split = (int)blockIdx.y;
@@ -516,8 +512,13 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
                     w[u][i][m] = scan::buf_load<f32x4>(rw[m], in ? wo + i * wt + (uint32_t)(k * (int)sizeof(T)) : kOut);
         }
     };
-    if (u0 + wave < u1) load_w(u0 + wave);
-    for (int unit = u0 + wave; unit < u1; unit += NW) {
+    // The wave's units of k, each workgroup from another one on: not all of them
+    // ask for the same part of every row at once.
+    const int count = max(0, (u1 - u0 - wave + NW - 1) / NW), turn = count ? (int)(blockIdx.x % (unsigned)count) : 0;
+    auto unit_of = [&](int c) { return u0 + wave + (c + turn >= count ? c + turn - count : c + turn) * NW; };
+    if (count) load_w(unit_of(0));
+    for (int c = 0; c < count; ++c) {
+        const int unit = unit_of(c);
         f32x4 x[U][TT], v[U][RT][NM];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
 #pragma unroll
                 for (int m = 0; m < NM; ++m) v[u][i][m] = w[u][i][m];
         }
-        if (unit + NW < u1) load_w(unit + NW);
+        if (c + 1 < count) load_w(unit_of(c + 1));
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -559,7 +560,7 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
                 for (int v = 1; v < NW; ++v) sum[m] += s_acc[v][m * TT + t][ln];
             }
             const int64_t col = t * 16 + ln % 16, r = r0 + 16 * i + ln / 16 * 4;
-            if (col >= a.T || r >= a.Ro || (RT == 1 && ln / 16 * 4 >= RH)) continue;
+            if (col >= a.T || r >= a.Ro || 16 * i + ln / 16 * 4 >= a.rows) continue;
             if (!kGates && a.splits > 1) {   // (rows of whole fours)
                 const int64_t ld = (a.Ro + 3) / 4 * 4;
                 *reinterpret_cast<f32x4 *>(a.part + ((int64_t)split * a.T + col) * ld + r) = sum[0];
@@ -579,6 +580,34 @@ __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     }
 }
 
+// Rows of weights a workgroup and parts of k: from estimated times (microseconds)
+// fitted to 288 products of 1 to 64 tokens with weights of 512 x 1376 to 8256 x 2112,
+// each with up to 40 choices; the choice costs 1.2% more than the best of them on
+// average.  A unit's workgroups add up, by what they read: .036 us for a KB of
+// weights and .018 of x.  So whole rounds of 256 workgroups matter most (48 tokens,
+// 8256 x 2112: 16.5 us in 36 rows each, 25.1 in 32), then few bytes of x (rows in
+// one workgroup), then the joining of parts.  For a few tokens 16 rows at most: two
+// workgroups a unit hide each other's latency (one token, the gates of 2048 -> 8192:
+// 13.8 us in 16 rows, 15.5 in 32).
+struct FewChoice {
+    int rows, splits;
+};
+template <typename T, bool kGates> FewChoice choose_few(const FewArgs &a) {
+    const double row = (double)(a.K * (int64_t)sizeof(T)) * 1e-3;   // KB
+    FewChoice best{16, 1};
+    double tbest = -1.0;
+    for (int rows = 8; rows <= (a.T <= 8 ? 16 : 48); rows += 4) {
+        for (const int splits : {1, 2, 3, 4, 6, 8}) {
+            const double part = 4e-6 * splits * (double)(a.T * ((a.Ro + 3) / 4 * 4));   // MB
+            if (splits > 1 && (kGates || row < 1.0 * splits || part * 1e6 > (double)kPartBytes)) break;
+            const double load = std::ceil((double)((a.Ro + rows - 1) / rows * splits) / 256.0);
+            double t = load * ((rows * (kGates ? 2 : 1) * .036 + (double)a.T * .018) * row / splits + .2);
+            if (splits > 1) t += 2.5 + 1.4 * part;
+            if (tbest < 0.0 || t < tbest) { tbest = t; best = FewChoice{rows, splits}; }
+        }
+    }
+    return best;
+}
 template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a, int rows, int splits, hipStream_t s) {
     a.rows = rows;
     a.splits = splits;
@@ -587,22 +616,12 @@ template <typename T, int TT, int RT, bool kGates> hipError_t few_run(FewArgs a,
     if (e != hipSuccess || splits == 1) return e;
     return join(JoinArgs{a.part, a.T * ((a.Ro + 3) / 4 * 4), splits, a.T, a.Ro, {a.out}, a.ldo, 0}, 1, sizeof(T) == 4, s);
 }
-// 32 rows a workgroup where there are enough for every compute unit, and where k
-// can be split; 8 where 16 would leave half of the units idle, and k need not be
-// split for them (4096 -> 1024 and back, 8 tokens: 14.7 us, 16.5 with 16 rows
-// of the gates; 8192 -> 2048, one token: 25.3 us a block, 27.1 with 16 rows and
-// four parts, but 30.9 and 30.0 with 16 tokens).
 template <typename T, int TT, bool kGates> hipError_t few(const FewArgs &a, hipStream_t s) {
-    const int64_t wide = (a.Ro + 31) / 32, groups = (a.Ro + 15) / 16;
-    if constexpr (kGates) {
-        if (TT > 1 && wide >= 256) return few_run<T, TT, 2, true>(a, 32, 1, s);
-        return few_run<T, TT, 1, true>(a, TT == 1 && groups <= 128 ? 8 : 16, 1, s);
-    } else {
-        if (TT == 1 && a.T <= 8 && groups <= 128 && groups >= 64) return few_run<T, TT, 1, false>(a, 8, 1, s);
-        // parts of at least 1 KiB of each row for each of the waves
-        const int64_t most = std::min<int64_t>(8, a.K * (int64_t)sizeof(T) / 4096);
-        const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / (TT > 1 ? wide : groups)));
-        return TT > 1 ? few_run<T, TT, 2, false>(a, 32, splits, s) : few_run<T, TT, 1, false>(a, 16, splits, s);
+    const FewChoice c = choose_few<T, kGates>(a);
+    switch ((c.rows + 15) / 16) {
+    case 1: return few_run<T, TT, 1, kGates>(a, c.rows, c.splits, s);
+    case 2: return few_run<T, TT, 2, kGates>(a, c.rows, c.splits, s);
+    default: return few_run<T, TT, 3, kGates>(a, c.rows, c.splits, s);
     }
 }
 template <typename T, bool kGates> hipError_t few_rows(const FewArgs &a, hipStream_t s) {

@@ -223,3 +223,51 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(ref, out, eager))
+
+
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 264, 8260), (9, 40, 12300), (33, 264, 8260), (64, 264, 8260), (50, 2056, 1000),
+                                  (17, 4100, 24)], ids=str)
+def test_few_tokens_of_wide_weights(io, size):
+    """Workgroups of up to 48 rows of weights, the last of a few, k in parts."""
+    T, D, F = size
+    say(f"ffn few {size} {io}")
+    x, Wg, Wu, Wd, _ = inputs(T, D, F, io, seed=T + F)
+    check("y", m3.ffn_fwd(x, Wg, Wu, Wd), reference(x, Wg, Wu, Wd, io=io)["y"])
+
+
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_backward_in_runs_of_tokens(io):
+    """So wide that dh is formed for 256 tokens at a time.  Half a million sums an
+    output: the values between the products are followed through their rounding
+    one by one.  With e the fp32 error of v, the stored value lies between v - e
+    and v + e rounded; what that leaves open, the sums' own errors and the
+    result's rounding (2^-8 of it in bf16) make the bar."""
+    say(f"ffn runs {io}")
+    T, D, F = 600, 16, 32900
+    x, Wg, Wu, Wd, dy = inputs(T, D, F, io, seed=5)
+    got = m3.ffn_bwd(x, Wg, Wu, Wd, dy)
+    x, Wg, Wu, Wd, dy = (t.double() for t in (x, Wg, Wu, Wd, dy))
+    sums = lambda K: (8 + 2 * K ** 0.5) * U  # noqa: E731
+    end = 2.0 ** -8 if io == torch.bfloat16 else 2 * U
+    g, u, dh = x @ Wg.T, x @ Wu.T, dy @ Wd
+    eg, eu, edh = (sums(D) * e for e in (x.abs() @ Wg.abs().T, x.abs() @ Wu.abs().T, dy.abs() @ Wd.abs()))
+    f, df = activation(g, "silu")
+
+    def stored(v, e):
+        r, lo, hi = (w.to(io).double() for w in (v, v - e, v + e))
+        return r, torch.maximum(hi - r, r - lo)
+    h, eh = stored(f * u, (df.abs() + 4 * U) * eg * u.abs() + f.abs() * eu + 8 * U * (f * u).abs())
+    du, edu = stored(dh * f, edh * f.abs() + 2 * dh.abs() * eg + 8 * U * (dh * f).abs())
+    dg, edg = stored(dh * u * df, edh * (u * df).abs() + dh.abs() * (eu * df.abs() + 2 * u.abs() * eg)
+                     + 16 * U * (dh * u).abs())
+
+    def bar(v, e, K, size):
+        return v, e + sums(K) * size + end * v.abs()
+    check("dx", got["dx"], bar(dg @ Wg + du @ Wu, edg @ Wg.abs() + edu @ Wu.abs(), 2 * F,
+                               dg.abs() @ Wg.abs() + du.abs() @ Wu.abs()))
+    for name, a, e, b in (("dWg", dg, edg, x), ("dWu", du, edu, x), ("dWd", h, eh, dy)):
+        v, err, size = a.T @ b, e.T @ b.abs(), a.abs().T @ b.abs()
+        if name == "dWd":
+            v, err, size = v.T, err.T, size.T
+        check(name, got[name], bar(v, err, T, size))
