@@ -641,17 +641,19 @@ template <typename T> __global__ __launch_bounds__(256) void k_pad(PadArgs g) {
     typedef T whole __attribute__((ext_vector_type(EL)));
     typedef T piece __attribute__((ext_vector_type(EL), aligned(sizeof(T))));
     const PadArgs::Copy &c = g.copy[blockIdx.z];
-    const int64_t row = blockIdx.x, k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * EL;
-    if (row >= c.rows || k >= c.dst_ld) return;
-    const T *src = static_cast<const T *>(c.src) + row * c.src_ld + k;
-    whole v;
-    if (k + EL <= c.cols) {
-        v = *reinterpret_cast<const piece *>(src);
-    } else {
+    const int64_t k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * EL;
+    if (k >= c.dst_ld) return;
+    for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
+        const T *src = static_cast<const T *>(c.src) + row * c.src_ld + k;
+        whole v;
+        if (k + EL <= c.cols) {
+            v = *reinterpret_cast<const piece *>(src);
+        } else {
 #pragma unroll
-        for (int e = 0; e < EL; ++e) v[e] = k + e < c.cols ? src[e] : (T)0.f;
+            for (int e = 0; e < EL; ++e) v[e] = k + e < c.cols ? src[e] : (T)0.f;
+        }
+        *reinterpret_cast<whole *>(static_cast<T *>(c.dst) + row * c.dst_ld + k) = v;
     }
-    *reinterpret_cast<whole *>(static_cast<T *>(c.dst) + row * c.dst_ld + k) = v;
 }
 
 int64_t part_elements(const GemmArgs &g) {
@@ -752,7 +754,8 @@ hipError_t launch_pad(const PadArgs &g, bool f32, hipStream_t s) {
         cols = std::max(cols, g.copy[k].dst_ld);
     }
     if (rows == 0) return hipSuccess;
-    const dim3 grid((unsigned)rows, (unsigned)((cols * (f32 ? 4 : 2) + 4095) / 4096), (unsigned)g.count), block(256);
+    // (a launch holds fewer than 2^32 threads)
+    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 16), (unsigned)((cols * (f32 ? 4 : 2) + 4095) / 4096), (unsigned)g.count), block(256);
     if (f32) k_pad<float><<<grid, block, 0, s>>>(g);
     else k_pad<bf16><<<grid, block, 0, s>>>(g);
     return hipGetLastError();

@@ -271,3 +271,13 @@ def test_backward_in_runs_of_tokens(io):
         if name == "dWd":
             v, err, size = v.T, err.T, size.T
         check(name, got[name], bar(v, err, T, size))
+
+
+def test_more_rows_to_copy_than_workgroups():
+    """Rows of an odd width, copied: more of them than the copy has workgroups."""
+    say("ffn 70001 rows of 3")
+    x, Wg, Wu, Wd, dy = inputs(70001, 3, 5, torch.float32, 9)
+    y, ref = m3.ffn_fwd(x, Wg, Wu, Wd), reference(x, Wg, Wu, Wd, dy)
+    check("y", y, ref["y"])
+    for name, got in m3.ffn_bwd(x, Wg, Wu, Wd, dy).items():
+        check(name, got, ref[name])
