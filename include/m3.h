@@ -512,8 +512,9 @@ void m3_set_wait_limit(uint32_t polls);
  * `states`: dx, dr, di and, with z, dz (contiguous, io dtype), dA [width]
  * (summed over batch and tokens in fp64 from fp32 parts), and with
  * dinit_state not NULL the initial state's, [batch][width].  Everything is
- * overwritten.  Where a_t rounds to 1 the derivative of sqrt(1 - a_t^2) has
- * no finite value; its products in dr and dA tend to zero and are taken so.
+ * overwritten.  Where 1 - a_t^2 is below 2^-126 (a nearly closed gate) that
+ * factor and what its derivative adds to dr and dA, which goes to zero with
+ * rho_t, are taken as zero.
  *
  * m3_glr_step: one token; x, r, i and z [batch][width] (batch strides; the
  * token strides and seqlen are ignored), state updated in place, y

@@ -379,8 +379,10 @@ __global__ __launch_bounds__(kFwdWaves * 64, 4) void k_fwd(FwdArgs a) {
 //     dx = g w iota,  di = g w x iota (1 - iota),  dz = dy h SiLU'(z)
 //     dlog a = a g h_{t-1} - (a^2 / w) g iota x
 //     dr = A dlog a rho (1 - rho),  dA = sum rho dlog a
-// At w = 0 (a = 1: rho has underflowed) the second term of dlog a is taken as
-// zero: multiplied by rho, as in dr and dA, it goes to zero there.
+// Where 1 - a^2 is below fp32's smallest normal number, 2^-126 (rho has all but
+// underflowed), w and the second term of dlog a are taken as zero: w is at most
+// 1.1e-19 there, and the term, multiplied by rho as in dr and dA, goes to zero with
+// it.  (The hardware's root and its reciprocal read a subnormal number as zero.)
 template <typename T, int V, bool kGate>
 __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
     typedef typename Raw<T, V>::type R;
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
             const float x = get(vx[s], e), dy = get(vd[s], e), av = at[s][e], ig = iota[s][e];
             forget(rho[s][e]);   // (w is formed again)
             const float om = one_minus_square(av, A2[e] * rho[s][e]);
-            const float iw = om > 0.f ? __builtin_amdgcn_rsqf(om) : 0.f, w = om * iw;
+            const float iw = om >= 0x1p-126f ? __builtin_amdgcn_rsqf(om) : 0.f, w = om * iw;
             float dh = dy;
             if constexpr (kGate) {
                 const float z = get(vz[s], e), sz = sigmoid(z), gz = z * sz;

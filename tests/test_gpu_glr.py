@@ -194,6 +194,45 @@ def test_closed_gates_and_resets():
     assert ((y.double() - ref).abs() <= 8 * U * ref.abs()).all()
 
 
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("gate", [False, True])
+def test_nearly_closed_gates(io, gate):
+    """r from -82 to -90, where 1 - a^2 goes below the smallest normal number before
+    rho is zero: everything is finite and as the definition gives it."""
+    say(f"glr nearly closed {io} gate={gate}")
+    decays = [0.005, 0.0066, 0.02, 0.05, 0.1, 0.3, 0.5, 1.0]
+    B, L, D = 2, 200, len(decays)
+    s = inputs(B, L, D, io, gate, 21)
+    s["A"] = -torch.tensor(decays, device=DEV)
+    s["r"][:, 60:125] = torch.linspace(-82.0, -90.0, 65, device=DEV).to(io)[:, None]
+    s["r"][:, 150] = -86.0
+    close.io = io
+    args = (s["x"], s["r"], s["i"], s["A"])
+    y, fs, st = m3.glr_fwd(*args, z=s["z"], init_state=s["h0"], save_states=True)
+    g = m3.glr_bwd(*args, st, s["dy"], z=s["z"], dfinal=s["dfinal"], want_dinit=True)
+    state = fs.clone()
+    ys = m3.glr_step(state, *(s[k][:, 90] for k in ("x", "r", "i")), s["A"], z=None if s["z"] is None else s["z"][:, 90])
+    assert torch.isfinite(ys).all() and torch.equal(state, fs)     # (w iota x is below a rounding)
+    ref = reference(**s)
+    close("y", y, ref["y"], L)
+    close("final", fs, ref["final"], L)
+    for k in ("dx", "dr", "di", *(("dz",) if gate else ())):
+        close(k, g[k], ref[k], L)
+    close("dA", g["dA"], ref["dA"], L, scale=ref["A_terms"])
+    close("dinit", g["dinit"], ref["dinit"], L)
+
+
+def test_decays_of_almost_nothing():
+    """Decays so small that 1 - a^2 is below the smallest normal number at any gate: the
+    state passes through, and no gradient is infinite."""
+    s = inputs(2, 300, 6, torch.float32, True, 22)
+    s["A"] = -torch.tensor([0.0, 1e-45, 1e-40, 1e-39, 5e-39, 1e-38], device=DEV)
+    y, fs, st = m3.glr_fwd(s["x"], s["r"], s["i"], s["A"], init_state=s["h0"], save_states=True)
+    g = m3.glr_bwd(s["x"], s["r"], s["i"], s["A"], st, s["dy"], dfinal=s["dfinal"], want_dinit=True)
+    assert ((fs - s["h0"]).abs() <= 300 * 1.5e-19 * s["x"].abs().max() + U * s["h0"].abs()).all()
+    assert all(torch.isfinite(v).all() for v in g.values())
+
+
 def test_nonfinite_inputs_stay_in_their_channel_and_later():
     s = inputs(2, 700, 40, torch.bfloat16, False, 6)
     clean, _ = m3.glr_fwd(s["x"], s["r"], s["i"], s["A"], init_state=s["h0"])
