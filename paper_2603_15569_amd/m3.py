@@ -1,7 +1,9 @@
 """Python binding of libm3 (ctypes): argument marshalling only.
 
 Every step of the path runs in the HIP kernels behind the C ABI declared in
-include/m3.h; PyTorch supplies device memory and the current HIP stream.
+include/m3.h; PyTorch supplies device memory and the current HIP stream.  A call
+given another `stream` behaves as under torch.cuda.stream(stream): what it
+allocates belongs to that stream, and the inputs have to be ready there.
 There is no fallback: when libm3.so is missing or a call fails, an exception
 is raised.
 """
@@ -200,6 +202,22 @@ def _stream(stream) -> int:
             return _raw_stream(_cur_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _on_stream(stream, call, *args):
+    """call(*args) as it runs where `stream` is the current one: what it allocates and
+    clears is in that stream's order, not in the caller's.  Its results may be used on
+    the caller's stream once that has waited, and freed there."""
+    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+    here = torch.cuda.current_stream()
+    if s.cuda_stream == here.cuda_stream:
+        return call(*args)
+    with torch.cuda.stream(s):
+        out = call(*args)
+    for t in out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(here)
+    return out
 
 
 def _a_strides(A: torch.Tensor, batch: int, seqlen: int, nheads: int):
@@ -674,6 +692,8 @@ def glr_fwd(x, r, i, A, z=None, init_state=None, save_states: bool = False, out=
     fp32, channels next to each other, any batch and token strides), A [D] fp32.
     Returns y [B, L, D], final_state [B, D] fp32 and, with `save_states`, the states
     that glr_bwd takes.  `out` may supply (y, final_state)."""
+    if stream is not None and (out is None or workspace is None or save_states):
+        return _on_stream(stream, glr_fwd, x, r, i, A, z, init_state, save_states, out, workspace)
     y, fs = (None, None) if out is None else out
     B, L, D = x.shape
     d = _glr_call(_meta(x), _meta(r), _meta(i), _meta(z), _meta(A), _meta(y), None, _meta(init_state), _meta(fs))
@@ -693,6 +713,8 @@ def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = Fals
     """m3_glr_bwd: gradients of J = <dy, y> + <dfinal, final_state>, from the forward's
     inputs and the states it saved.  Returns a dict: dx, dr, di (dz) in the io dtype,
     dA [D] fp32 and, with `want_dinit`, dinit [B, D] fp32."""
+    if stream is not None:
+        return _on_stream(stream, glr_bwd, x, r, i, A, states, dy, z, dfinal, want_dinit, workspace)
     B, _, D = x.shape
     if states is None or dy is None:
         raise ValueError("glr_bwd takes the forward's states and dy")
@@ -715,6 +737,8 @@ def glr_bwd(x, r, i, A, states, dy, z=None, dfinal=None, want_dinit: bool = Fals
 def glr_step(state, x, r, i, A, z=None, y=None, stream=None):
     """m3_glr_step: one token, x, r, i, z [B, D]; advances `state` [B, D] fp32 in
     place and returns y [B, D]."""
+    if stream is not None and y is None:
+        return _on_stream(stream, glr_step, state, x, r, i, A, z)
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D], got {tuple(x.shape)}")
     d = _glr_call(_meta(x), _meta(r), _meta(i), _meta(z), _meta(A), _meta(y), None, _meta(state))
@@ -776,6 +800,8 @@ def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=N
     """m3_ffn_fwd: y = (act(x Wg^T) o (x Wu^T)) Wd^T; x [..., D] (rows at one stride), Wg
     and Wu [F, D], Wd [D, F], bf16 or fp32; act "silu" or "gelu" (tanh form).  Returns
     y, shaped like x, contiguous."""
+    if stream is not None and (out is None or workspace is None):
+        return _on_stream(stream, ffn_fwd, x, Wg, Wu, Wd, act, out, workspace)
     d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), _meta(out), None, act)
     y = out if out is not None else _empty(x)
     if workspace is None:
@@ -788,6 +814,8 @@ def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=N
 def ffn_bwd(x, Wg, Wu, Wd, dy, act: str = "silu", workspace=None, stream=None):
     """m3_ffn_bwd: gradients of J = <dy, y> from the forward's inputs (g and u are formed
     again).  Returns a dict: dx (shaped like x), dWg, dWu, dWd, in the io dtype."""
+    if stream is not None:
+        return _on_stream(stream, ffn_bwd, x, Wg, Wu, Wd, dy, act, workspace)
     d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), None, _meta(dy), act)
     out = dict(dx=_empty(x), dWg=_empty(Wg), dWu=_empty(Wu), dWd=_empty(Wd))
     if workspace is None:

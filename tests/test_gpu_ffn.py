@@ -281,3 +281,18 @@ def test_more_rows_to_copy_than_workgroups():
     check("y", y, ref["y"])
     for name, got in m3.ffn_bwd(x, Wg, Wu, Wd, dy).items():
         check(name, got, ref[name])
+
+
+def test_given_stream_without_a_workspace():
+    """`stream` as an argument: workspace and outputs are in that stream's order."""
+    x, Wg, Wu, Wd, dy = inputs(300, 256, 704, torch.bfloat16, 6)
+    both = lambda **kw: [m3.ffn_fwd(x, Wg, Wu, Wd, **kw), *m3.ffn_bwd(x, Wg, Wu, Wd, dy, **kw).values()]  # noqa: E731
+    ref = both()
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    side.wait_stream(here)
+    for _ in range(3):
+        got = both(stream=side)
+        busy = torch.full((64 << 20,), 171, dtype=torch.uint8, device=DEV)   # (memory that a call gave back too early)
+        here.wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(ref, got))
+        del busy

@@ -308,3 +308,30 @@ def test_wait_that_gives_up_is_counted_and_leaves_nan():
     assert n > 0 and torch.isnan(fs).any() and torch.isnan(y).any()
     again, _ = m3.glr_fwd(*args, workspace=ws)
     assert m3.glr_check(s["x"], s["r"], s["i"], ws) == 0 and torch.equal(again, ref)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_given_stream_without_a_workspace(raw):
+    """`stream` as an argument, nothing else given: the workspace's clearing and the
+    outputs are in that stream's order, whatever their memory held before and however
+    long the current stream is at work."""
+    s = inputs(2, 3000, 192, torch.bfloat16, True, 17)
+    args = (s["x"], s["r"], s["i"], s["A"])
+
+    def both(**kw):
+        y, fs, st = m3.glr_fwd(*args, z=s["z"], init_state=s["h0"], save_states=True, **kw)
+        return [y, fs, st, *m3.glr_bwd(*args, st, s["dy"], z=s["z"], dfinal=s["dfinal"], want_dinit=True, **kw).values()]
+    ref = both()
+    n = m3.glr_workspace(s["x"], s["r"], s["i"], z=s["z"]).numel()
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    work = torch.randn(4096, 4096, device=DEV)
+    for _ in range(3):
+        side.wait_stream(here)
+        for st in (here, side):       # both streams' free memory full of other values
+            with torch.cuda.stream(st):
+                junk = [torch.full((m,), 171, dtype=torch.uint8, device=DEV) for m in (n, 2 * n, 16 << 20)]
+                del junk
+        work = work @ work * 1e-3     # (the current stream is behind)
+        got = both(stream=side.cuda_stream if raw else side)
+        here.wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(ref, got))

@@ -252,6 +252,42 @@ def test_binding_refuses_host_tensors():
             call()
 
 
+@pytest.mark.parametrize("raw", [False, True])
+def test_a_given_stream_orders_what_a_call_allocates(two_streams, raw):
+    """With `stream` another than the current one, outputs, workspaces and their clearing
+    are in the given stream's order (the kernels read the cleared workspace), and the
+    outputs are kept for the caller's."""
+    here, side, log = two_streams
+    s = side.cuda_stream if raw else side
+    x, A = torch.zeros(2, 5, 8, dtype=torch.bfloat16), -torch.ones(8)
+    W, Wd = torch.zeros(12, 8, dtype=torch.bfloat16), torch.zeros(8, 12, dtype=torch.bfloat16)
+    states, one = torch.zeros(2, 1, 8), torch.zeros(2, 8, dtype=torch.bfloat16)
+    for call in (lambda: m3.glr_fwd(x, x, x, A, save_states=True, stream=s), lambda: m3.glr_bwd(x, x, x, A, states, x, stream=s),
+                 lambda: m3.glr_step(torch.ones(2, 8), one, one, one, A, stream=s),
+                 lambda: m3.ffn_fwd(x, W, W, Wd, stream=s), lambda: m3.ffn_bwd(x, W, W, Wd, x, stream=s)):
+        log.clear()
+        out = call()
+        out = list(out.values()) if isinstance(out, dict) else list(out) if isinstance(out, tuple) else [out]
+        ran = [e for e in log if e[0] != "kept for"]
+        assert ran[-1][0].startswith("m3_") and len(ran) >= 2
+        assert all(e[1] == side.cuda_stream and e[2] == side.cuda_stream for e in ran), ran
+        assert sorted(e[2] for e in log if e[0] == "kept for") == sorted(t.data_ptr() for t in out)
+        assert all(e[1] == here.cuda_stream for e in log if e[0] == "kept for")
+
+
+def test_a_given_stream_with_everything_supplied(two_streams):
+    """Nothing to allocate: the call goes straight to the given stream."""
+    here, side, log = two_streams
+    x, A, y, fs = torch.zeros(2, 5, 8), -torch.ones(8), torch.zeros(2, 5, 8), torch.zeros(2, 8)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    log.clear()
+    m3.glr_fwd(x, x, x, A, out=(y, fs), workspace=ws, stream=side)
+    m3.glr_step(fs, x[:, 0].contiguous(), x[:, 0].contiguous(), x[:, 0].contiguous(), A, y=y[:, 0].contiguous(), stream=side)
+    m3.ffn_fwd(x, torch.ones(12, 8), torch.ones(12, 8), torch.ones(8, 12), out=y, workspace=ws, stream=side)
+    assert [e for e in log if e[0].startswith("m3_")] == [(n, 2, 1) for n in ("m3_glr_fwd", "m3_glr_step", "m3_ffn_fwd")]
+    assert not [e for e in log if e[0] in ("empty", "empty_like", "kept for")]
+
+
 @pytest.mark.gpu
 def test_binding_refuses_workspaces_and_scalars_elsewhere():
     x, A = torch.zeros(2, 5, 8, dtype=torch.bfloat16, device="cuda"), -torch.ones(8, device="cuda")
