@@ -214,8 +214,9 @@ def _on_stream(stream, call, *args):
         return call(*args)
     with torch.cuda.stream(s):
         out = call(*args)
-    for t in out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,):
-        if t is not None:
+    results = out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,)
+    for r in results:
+        for t in r if isinstance(r, tuple) else (r,):     # (a carry is a pair)
             t.record_stream(here)
     return out
 
@@ -286,6 +287,9 @@ def scan_fwd(x, Bm, Cm, dt, A, lam, theta, D, chunk: int,
     per workgroup), else the segmented kernel with `seg` chunks per
     workgroup (0: library choice).  With `check`, the call synchronises and
     raises LookBackTimeout when a look-back wait gave up (m3_scan_check)."""
+    if stream is not None and (out is None or workspace is None):
+        return _on_stream(stream, scan_fwd, x, Bm, Cm, dt, A, lam, theta, D, chunk, init_state, init_carry,
+                          out, workspace, None, split, per_chunk, seg, z, check)
     d = scan_dims(x, Bm, chunk, A, split, per_chunk, seg,
                   _theta_per_head(theta, x.shape[2], Bm.shape[-1]))
     batch, seqlen, nheads, rank, headdim = x.shape
@@ -388,6 +392,9 @@ def scan_fwd_varlen(x, Bm, Cm, dt, A, lam, theta, D, chunk: int, cu_seqlens,
     y [T,H,R,P], final_state [S,H,N,P] and the carry ([S,H,R,N], [S,H,R,P]).
     Without a workspace one is allocated (zero-filled) for the one-launch
     scan where that applies, else for the largest sequence."""
+    if stream is not None:
+        return _on_stream(stream, scan_fwd_varlen, x, Bm, Cm, dt, A, lam, theta, D, chunk, cu_seqlens,
+                          init_state, init_carry, z, workspace, None, split, per_chunk, seg, check)
     cu = [int(v) for v in (cu_seqlens.tolist() if hasattr(cu_seqlens, "tolist") else cu_seqlens)]
     T, nheads, rank, headdim = x.shape
     dstate = Bm.shape[-1]
@@ -454,6 +461,8 @@ def step(state, carry, x_t, B_t, C_t, dt_t, A, lam_t, theta_t, D, y=None, stream
     given: y_t o SiLU(z_t); `theta_t` [B,H,N/2] angles or [H,N/2] frequencies
     omega, as in scan_fwd): advances `state` [B,H,N,P] and `carry`
     (B [B,H,R,N], X [B,H,R,P]) in place by one token; returns y_t [B,H,R,P]."""
+    if stream is not None and y is None:
+        return _on_stream(stream, step, state, carry, x_t, B_t, C_t, dt_t, A, lam_t, theta_t, D, None, None, z)
     xs, bs = x_t.shape, B_t.shape
     d = _step_dims(xs, bs, x_t.dtype, A.shape, A.stride(), _theta_per_head(theta_t, xs[1], bs[-1]))
     if y is None:
@@ -496,6 +505,9 @@ def scan_fwd_pro(x, Bm, Cm, dt, A, lam, theta, D, chunk: int, pro: M3Prologue, r
     state and the carry (the prologue's B_{L-1}, X_{L-1}).  `seg` is the
     dims' seg_chunks (0: chosen at launch; at least the chunk count: one
     segment per slice, the warp-specialised kernel where it is built)."""
+    if stream is not None and (out is None or workspace is None):
+        return _on_stream(stream, scan_fwd_pro, x, Bm, Cm, dt, A, lam, theta, D, chunk, pro, rank, z,
+                          init_state, init_carry, out, workspace, None, check, seg)
     batch, seqlen, nheads = x.shape[:3]
     headdim, dstate = x.shape[-1], Bm.shape[-1]
     if tuple(Bm.shape) != (batch, seqlen, nheads, rank, dstate):
@@ -532,6 +544,8 @@ def step_pro(state, carry, x_t, B_t, C_t, dt_t, A, lam_t, theta_t, D, pro: M3Pro
              z=None, y=None, stream=None):
     """m3_step_pro: one decode step with the block prologue; x_t (z) is
     [B,H,P] when pro.w_x (pro.w_z) is set.  Returns y_t [B,H,R,P]."""
+    if stream is not None and y is None:
+        return _on_stream(stream, step_pro, state, carry, x_t, B_t, C_t, dt_t, A, lam_t, theta_t, D, pro, z)
     batch, nheads, rank, dstate = B_t.shape
     headdim = x_t.shape[-1]
     if A.dim() == 1 and A.shape[0] == nheads:
@@ -557,6 +571,9 @@ def scan_bwd(x, Bm, Cm, dt, A, lam, theta, D, dy, chunk: int, dfinal=None, init_
     scan of these inputs.  Returns a dict: dx, dB, dC (io dtype), ddt, dlam,
     dtheta, dD, dA ([H] for a per-head A, [B,L,H] for a per-token A) and
     dinit (when `want_dinit`)."""
+    if stream is not None:
+        return _on_stream(stream, scan_bwd, x, Bm, Cm, dt, A, lam, theta, D, dy, chunk, dfinal, init_state,
+                          want_dinit, workspace)
     d = scan_dims(x, Bm, chunk, A)
     batch, seqlen, nheads, rank, headdim = x.shape
     dstate = Bm.shape[-1]

@@ -1230,3 +1230,30 @@ def test_nan_token_reach(N, R, Q, B_, H, L, what):
     assert torch.equal(y[0, :first, 1], want[0, :first, 1])
     y[0, :, 1], fs[0, 1] = want[0, :, 1], wfs[0, 1]
     assert torch.equal(y, want) and torch.equal(fs, wfs)
+
+
+@pytest.mark.parametrize("mode", ["seg", "per_chunk"])
+def test_given_stream_without_a_workspace(mode):
+    """`stream` as an argument, nothing else given: the workspace's clearing and the
+    outputs are in that stream's order, whatever their memory held before and however
+    long the current stream is at work."""
+    inp = make_scan_inputs(2, 2048, 2, 64, 128, 1, io="bf16", seed=5, device=DEV)
+    kw = dict(chunk=64, per_chunk=mode == "per_chunk", seg=4 if mode == "seg" else 0)
+
+    def run(**more):
+        y, fs, (cB, cX) = m3.scan_fwd(inp.x, inp.Bm, inp.Cm, inp.dt, inp.A, inp.lam, inp.theta, inp.D, **kw, **more)
+        return y, fs, cB, cX
+    ref = run()
+    n = m3.workspace_bytes(m3.scan_dims(inp.x, inp.Bm, 64, inp.A, per_chunk=mode == "per_chunk", seg=kw["seg"]))
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    work = torch.randn(4096, 4096, device=DEV)
+    for _ in range(3):
+        side.wait_stream(here)
+        for st in (here, side):       # both streams' free memory full of other values
+            with torch.cuda.stream(st):
+                junk = [torch.full((m,), 171, dtype=torch.uint8, device=DEV) for m in (n, 2 * n, 16 << 20)]
+                del junk
+        work = work @ work * 1e-3     # (the current stream is behind)
+        got = run(stream=side)
+        here.wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(ref, got))

@@ -401,3 +401,33 @@ def test_step_dims_by_shape_and_stride(L):
     assert m3.step_dims(x, B, torch.zeros(3)).batch == 2
     with pytest.raises(ValueError):
         m3.step_dims(x, B, torch.zeros(2))
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_a_given_stream_orders_what_a_scan_allocates(two_streams, raw):
+    """With `stream` another than the current one, the scans', the backward's and the
+    steps' outputs, workspaces and their clearing are in the given stream's order, and
+    the outputs are kept for the caller's."""
+    import torch
+
+    from paper_2603_15569_amd.inputs import make_scan_inputs
+    here, side, log = two_streams
+    s = side.cuda_stream if raw else side
+    a = make_scan_inputs(2, 8, 2, 16, 16, 1, io="bf16")
+    scan = (a.x, a.Bm, a.Cm, a.dt, a.A, a.lam, a.theta, a.D)
+    flat = [t.flatten(0, 1) if t.dim() > 2 else t for t in scan]
+    one = [t[:, 0].contiguous() if t.dim() > 2 else t for t in scan]
+    state, carry = torch.zeros(2, 2, 16, 16), (one[1].clone(), one[0].clone())
+    pro = m3.prologue()
+    for call in (lambda: m3.scan_fwd(*scan, chunk=8, stream=s), lambda: m3.scan_bwd(*scan, a.x, chunk=8, want_dinit=True, stream=s),
+                 lambda: m3.scan_fwd_varlen(*flat, chunk=8, cu_seqlens=[0, 5, 16], stream=s),
+                 lambda: m3.scan_fwd_pro(*scan, 8, pro, 1, stream=s),
+                 lambda: m3.step(state, carry, *one, stream=s), lambda: m3.step_pro(state, carry, *one, pro, stream=s)):
+        log.clear()
+        out = call()
+        out = list(out.values()) if isinstance(out, dict) else [*out[:2], *out[2]] if isinstance(out, tuple) else [out]
+        ran = [e for e in log if e[0] != "kept for"]
+        assert ran[-1][0].startswith("m3_") and len(ran) >= 2
+        assert all(e[1] == side.cuda_stream and e[2] == side.cuda_stream for e in ran), ran
+        assert sorted(e[2] for e in log if e[0] == "kept for") == sorted(t.data_ptr() for t in out)
+        assert all(e[1] == here.cuda_stream for e in log if e[0] == "kept for")
