@@ -126,6 +126,7 @@ __device__ __forceinline__ uint64_t get_word(const uint64_t *p) {
 __device__ __forceinline__ float word_value(uint64_t w) { return __uint_as_float((uint32_t)w); }
 
 struct Item {
+    bool none;      // no item: the workgroup leaves
     int tile;       // index of the tile in the order of its recurrence
     int b, grp;     // batch row, channel group
     uint32_t tag;
@@ -134,7 +135,9 @@ struct Item {
 // Work items in ticket order, tile-major: every tile that an item waits for
 // has an earlier ticket, so it is running or done.  The counter's upper half
 // is the count of calls on the workspace (plus one: the tag); whoever takes
-// the last ticket sets it up for the next call.
+// the last ticket sets it up for the next call.  A workspace that was not
+// cleared may hold any ticket: one past the items takes none, and is counted as
+// a wait that gave up (in both calls' words: the count of calls means nothing).
 __device__ __forceinline__ Item take_item(uint64_t *ctl, uint32_t B, uint32_t tiles, uint32_t G, uint64_t *s_ticket) {
     // (divisions leave their results in vector registers: back to scalar ones)
     auto scalar = [](uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); };
@@ -148,15 +151,18 @@ __device__ __forceinline__ Item take_item(uint64_t *ctl, uint32_t B, uint32_t ti
                                    __HIP_MEMORY_SCOPE_AGENT);
                 __hip_atomic_store(ctl, (uint64_t)(epoch + 1) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
+            if ((uint32_t)w >= B * G * tiles)
+                for (int e = 0; e < 2; ++e)
+                    __hip_atomic_fetch_add(reinterpret_cast<uint32_t *>(ctl) + 2 + e, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             *s_ticket = w;
         }
         __syncthreads();
         const uint64_t w = *s_ticket;
-        k = (uint32_t)w;
+        k = (uint32_t)scalar((uint32_t)w);
         tag = (uint32_t)(w >> 32) + 1u;
     }
     const uint32_t tile = k / (B * G), in = k - tile * (B * G), b = in / G;
-    return Item{scalar(tile), scalar(b), scalar(in - b * G), (uint32_t)scalar(tag)};
+    return Item{k >= B * G * tiles, scalar(tile), scalar(b), scalar(in - b * G), (uint32_t)scalar(tag)};
 }
 
 // Published words of a tile and channel: the state after the tile, and the
@@ -260,6 +266,7 @@ __global__ __launch_bounds__(kFwdWaves * 64, 4) void k_fwd(FwdArgs a) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Item it = take_item(a.ctl, (uint32_t)a.B, (uint32_t)a.tiles, (uint32_t)a.G, &s_ticket);
+    if (it.none) return;
     const int64_t d0 = (int64_t)it.grp * C + lane * V;
     const bool live = d0 < a.D;      // (V divides D)
     const int64_t dl = live ? d0 : 0;
@@ -393,6 +400,7 @@ __global__ __launch_bounds__(kBwdWaves * 64) void k_bwd(BwdArgs a) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Item it = take_item(a.ctl, (uint32_t)a.B, (uint32_t)a.tiles, (uint32_t)a.G, &s_ticket);
+    if (it.none) return;
     const int tile = (int)a.tiles - 1 - it.tile;    // in token order; it.tile counts from the end
     const int64_t d0 = (int64_t)it.grp * C + lane * V;
     const bool live = d0 < a.D;

@@ -335,3 +335,23 @@ def test_given_stream_without_a_workspace(raw):
         got = both(stream=side.cuda_stream if raw else side)
         here.wait_stream(side)
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+def test_tickets_past_the_items_do_nothing():
+    """A workspace whose ticket counter is not where a call left it: no workgroup writes
+    anything, and m3_glr_check says so; cleared, it serves again."""
+    s = inputs(2, 700, 48, torch.float32, False, 18)
+    args, dims = (s["x"], s["r"], s["i"], s["A"]), (s["x"], s["r"], s["i"])
+    ws = m3.glr_workspace(*dims)
+    ref = m3.glr_fwd(*args, workspace=ws)
+    for ticket in (2 * 6 * 1, 171, 0x7fffffff):      # (the call's items: 2 rows, 6 tiles, 1 group)
+        ws.zero_()
+        ws[:4].view(torch.int32)[0] = ticket
+        before = ws.clone()
+        y, fs = torch.full_like(s["x"], 7.0), torch.full((2, 48), 7.0, device=DEV)
+        m3.glr_fwd(*args, out=(y, fs), workspace=ws)
+        assert m3.glr_check(*dims, ws) == 12
+        assert (y == 7.0).all() and (fs == 7.0).all() and torch.equal(ws[16:], before[16:])
+    ws.zero_()
+    got = m3.glr_fwd(*args, workspace=ws)
+    assert m3.glr_check(*dims, ws) == 0 and all(torch.equal(a, b) for a, b in zip(ref, got))
