@@ -237,3 +237,40 @@ def test_many_tensors_on_a_side_stream_and_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert same()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+@pytest.mark.parametrize("gtype", [torch.float32, torch.bfloat16], ids=["gf32", "gbf16"])
+def test_small_gradients_without_eps(eight, gtype):
+    """Gradients of 1e-17 to 3e-21 on a zero state with eps = 0: v goes below the smallest
+    normal number, and the step is still the formula's, about lr.  A subnormal v is
+    known to three halves of 2^-149 (its square, its product and its sum), the step to
+    half of what that is of v; the rest as for every step."""
+    say(f"adamw small gradients eight={eight} {gtype}")
+    c = Case(11, eight, gtype, low=False, shapes=[(300,), (1025,)], zero=True)
+    total = c.flat["g"].numel()
+    gen = torch.Generator(DEV).manual_seed(4)
+    size = 10.0 ** (-17 - 3.5 * torch.rand(total, device=DEV, generator=gen, dtype=torch.float64))
+    sign = torch.randint(0, 2, (total,), device=DEV, generator=gen) * 2 - 1
+    c.flat["g"].copy_((size * sign).to(gtype))
+    lr, (b1, b2) = KW["lr"], KW["betas"]
+    want = []
+    for k in range(2):
+        g, p = c.views("g")[k].double(), c.views("p")[k].double()
+        v = (1 - b2) * g * g
+        upd = lr * g / g.abs()
+        off = 1.5 * 2.0 ** -149 / v
+        want.append((p - upd, 2 * U * p.abs() + upd.abs() * (28 * U + off), v.sqrt(), off))
+    m3.adamw_step(c.table, step=1, lr=lr, betas=(b1, b2), eps=0.0, seed=5)
+    for k, (p, bar, rv, off) in enumerate(want):
+        got = c.views("p")[k]
+        assert torch.isfinite(got).all() and ((got.double() - p).abs() <= bar).all(), k
+        if eight:
+            rows = torch.nn.functional.pad(rv, (0, -rv.numel() % BLOCK)).view(-1, BLOCK)
+            at = rows.argmax(1, keepdim=True)
+            most = rows.gather(1, at)[:, 0]
+            off = torch.nn.functional.pad(off, (0, -off.numel() % BLOCK)).view(-1, BLOCK).gather(1, at)[:, 0]
+            assert ((c.scales[k][:, 1].double() - most / 448).abs() <= (8 * U + off) * most / 448).all(), k
+            assert c.views("v")[k].float().gt(0).all()
+        else:
+            assert ((c.views("v")[k].double() - rv ** 2).abs() <= 4 * U * rv ** 2 + 1.5 * 2.0 ** -149).all(), k
