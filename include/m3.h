@@ -610,8 +610,15 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * bytes, 8-byte aligned; call with NULL first for the size).  The caller copies
  * the table to the device (16-byte aligned) and passes the plan and the device
  * copy to every step, as long as the tensors stay where they are.  n = 0 is
- * allowed.  m3_adamw_step launches nothing but the one kernel and copies
- * nothing, so it can be captured.
+ * allowed.  m3_adamw_step copies nothing and launches nothing but the one kernel
+ * (and one thread before it, with a number on the device), so it can be captured.
+ *
+ * A captured step keeps the config's numbers: each replay would be the same
+ * step t with the same lr and the same rounding.  With device_step not NULL, t is
+ * read from there when the kernels run (advance it between replays, or in the
+ * graph) and the rounding's seed is seed + t; with device_lr not NULL, lr too.  A
+ * t below 1 there gives NaN.  Such calls write to the table's end, so steps
+ * of one table follow one another, as they must anyway.
  *
  * 8-bit states (M3_ADAMW_8BIT): m and v hold e4m3 codes (1 byte an element) of
  * m and of sqrt(v), divided by scales[n / 256 rounded up][2] (fp32; m's, then
@@ -619,12 +626,12 @@ m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, con
  * scale, 0 where all are zero.  Zero codes with any scale are the zero state.
  * They are rounded stochastically with 16 bits each of a hash of the element's
  * index in its tensor and the low 32 bits of (seed + the tensor's place in the
- * list), so pass another seed for every step; a sqrt(v) that is not zero is
+ * list), so pass another seed for every step (device_step does so); a sqrt(v) that is not zero is
  * stored as at least the smallest code.  A non-finite gradient spoils its
  * block.
  * Pointers need their element's alignment only (else M3_ERR_ALIGN).  A NULL
  * list with count > 0, or a NULL pointer in a tensor with n > 0, is
- * M3_ERR_NULL; n < 0, step < 1, a beta outside [0, 1), eps < 0, or a lr, decay
+ * M3_ERR_NULL; n < 0, step < 1 (without device_step), a beta outside [0, 1), eps < 0, or a lr, decay
  * or eps that is not finite is M3_ERR_SHAPE; a table_bytes below the plan's
  * is M3_ERR_WORKSPACE.
  */
@@ -648,11 +655,13 @@ typedef struct {
     double lr, beta1, beta2, eps;
     int64_t step;       /* t >= 1                                            */
     uint64_t seed;
+    const int64_t *device_step;     /* device, 8-byte aligned; NULL: step    */
+    const double *device_lr;        /* device, 8-byte aligned; NULL: lr      */
 } m3_adamw_config;
 m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t count, int32_t grad_dtype,
                              int32_t flags, m3_adamw_plan *plan, void *host_table, size_t table_bytes);
 m3_status m3_adamw_step(const m3_adamw_config *config, const m3_adamw_plan *plan,
-                        const void *device_table, const float *grad_scale, void *stream);
+                        void *device_table, const float *grad_scale, void *stream);
 
 /* Static description of a status code. */
 const char *m3_status_string(m3_status status);

@@ -221,9 +221,11 @@ template <typename G, bool kEight>
 __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Tensor t = a.t[a.of[blockIdx.x]];
-    const float shrink = (float)(a.lr * t.decay);
-    const uint32_t seed = a.seed + t.index;
-    Step k{a.b1, a.c1, a.b2, a.c2, a.rate, a.root, a.eps, 1.f, a.grad_scale != nullptr};
+    Now now = a.now;
+    if (a.from) now = *a.from;
+    const float shrink = (float)(now.lr * t.decay);
+    const uint32_t seed = now.seed + t.index;
+    Step k{a.b1, a.c1, a.b2, a.c2, now.rate, now.root, a.eps, 1.f, a.grad_scale != nullptr};
     if (k.scaled) k.gs = *a.grad_scale;
     const int chunk = (int)blockIdx.x - t.first, first = wave * kBlockElems;
     const int left = min((chunk == t.chunks - 1 ? t.tail : kChunkElems) - first, kBlockElems);   // elements of this wave
@@ -233,8 +235,22 @@ __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     else block<G, kEight, false>(t, k, shrink, seed, base, left, lane);
 }
 
+// (one thread: the powers in fp64 for every wave would cost the 8-bit step its
+// spare time)
+__global__ void k_now(NowArgs a) {
+    const int64_t t = a.device_step ? *a.device_step : a.step;
+    const double lr = a.device_lr ? *a.device_lr : a.lr;
+    Now n = now(lr, a.beta1, a.beta2, t, a.seed + (a.device_step ? (uint64_t)t : 0));
+    if (t < 1) n.rate = __builtin_nanf("");
+    *a.to = n;
+}
+
 }  // namespace
 
+hipError_t launch_now(const NowArgs &a, hipStream_t s) {
+    k_now<<<dim3(1), dim3(1), 0, s>>>(a);
+    return hipGetLastError();
+}
 hipError_t launch(const Args &a, bool grad_f32, bool eight, hipStream_t s) {
     const dim3 grid((unsigned)a.groups), blk(kWaves * 64);
     if (grad_f32 && eight) k_adamw<float, true><<<grid, blk, 0, s>>>(a);

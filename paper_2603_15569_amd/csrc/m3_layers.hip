@@ -384,6 +384,11 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
 // AdamW
 // ---------------------------------------------------------------------------
 
+// Where a table's Now is
+static size_t now_at(int64_t rows, int64_t groups) {
+    return round_up((size_t)rows * sizeof(adamw::Tensor) + (size_t)groups * sizeof(int32_t), 16);
+}
+
 extern "C" m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t count, int32_t grad_dtype, int32_t flags,
                                         m3_adamw_plan *plan, void *host_table, size_t table_bytes) {
     if (!plan || (count > 0 && !tensors)) return M3_ERR_NULL;
@@ -404,7 +409,7 @@ extern "C" m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t 
         if (groups > 2 * kMostGroups) return M3_ERR_SHAPE;
         ++rows;
     }
-    const size_t head = (size_t)rows * sizeof(adamw::Tensor), bytes = round_up(head + (size_t)groups * sizeof(int32_t), 16);
+    const size_t head = (size_t)rows * sizeof(adamw::Tensor), bytes = now_at(rows, groups) + sizeof(adamw::Now);
     if (host_table) {
         if (table_bytes < bytes) return M3_ERR_WORKSPACE;
         if (!aligned(host_table, 8)) return M3_ERR_ALIGN;
@@ -425,28 +430,34 @@ extern "C" m3_status m3_adamw_plan_make(const m3_adamw_tensor *tensors, int64_t 
     return M3_OK;
 }
 
-extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_plan *plan, const void *table,
+extern "C" m3_status m3_adamw_step(const m3_adamw_config *c, const m3_adamw_plan *plan, void *table,
                                    const float *grad_scale, void *stream) {
     if (!c || !plan || (plan->groups > 0 && !table)) return M3_ERR_NULL;
     if (plan->grad_dtype != M3_F32 && plan->grad_dtype != M3_BF16) return M3_ERR_DTYPE;
     if (plan->rows < 0 || plan->rows > plan->groups || plan->groups > 2 * kMostGroups || (plan->flags & ~M3_ADAMW_8BIT) ||
-        c->step < 1)
+        (!c->device_step && c->step < 1))
         return M3_ERR_SHAPE;
-    if (!std::isfinite(c->lr) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) ||
+    if ((!c->device_lr && !std::isfinite(c->lr)) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) ||
         !(c->eps >= 0.0) || !std::isfinite(c->eps))
         return M3_ERR_SHAPE;
-    if (!aligned(grad_scale, 4) || !aligned(table, 16)) return M3_ERR_ALIGN;
+    if (!aligned(grad_scale, 4) || !aligned(table, 16) || !aligned(c->device_step, 8) || !aligned(c->device_lr, 8)) return M3_ERR_ALIGN;
     if (plan->groups == 0) return M3_OK;
-    adamw::Args a;
+    adamw::Args a = {};
     a.t = static_cast<const adamw::Tensor *>(table);
     a.of = reinterpret_cast<const int32_t *>(a.t + plan->rows);
     a.groups = (int32_t)plan->groups;
-    a.lr = c->lr;
-    a.seed = (uint32_t)c->seed;
-    const double bc1 = 1.0 - std::pow(c->beta1, (double)c->step), bc2 = 1.0 - std::pow(c->beta2, (double)c->step);
     a.b1 = (float)c->beta1; a.c1 = (float)(1.0 - c->beta1);
     a.b2 = (float)c->beta2; a.c2 = (float)(1.0 - c->beta2);
-    a.rate = (float)(c->lr / bc1); a.root = (float)std::pow(bc2, -0.5); a.eps = (float)c->eps;
+    a.eps = (float)c->eps;
     a.grad_scale = grad_scale;
+    if (c->device_step || c->device_lr) {
+        adamw::Now *now = reinterpret_cast<adamw::Now *>(static_cast<char *>(table) + now_at(plan->rows, plan->groups));
+        a.from = now;
+        const hipError_t e = adamw::launch_now(adamw::NowArgs{now, c->lr, c->beta1, c->beta2, c->step, c->seed, c->device_step, c->device_lr},
+                                               static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return launched(e);
+    } else {
+        a.now = adamw::now(c->lr, c->beta1, c->beta2, c->step, c->seed);
+    }
     return launched(adamw::launch(a, plan->grad_dtype == M3_F32, (plan->flags & M3_ADAMW_8BIT) != 0, static_cast<hipStream_t>(stream)));
 }

@@ -78,7 +78,8 @@ class M3AdamwTensor(ctypes.Structure):
 
 class M3AdamwConfig(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("device_step", ctypes.c_void_p), ("device_lr", ctypes.c_void_p)]
 
 
 class M3AdamwPlan(ctypes.Structure):
@@ -898,17 +899,32 @@ def adamw_table(params, grads, exp_avg, exp_avg_sq, weight_decay=0.0, low=None, 
     return AdamWTable(plan, host.to(dev), held)
 
 
-def adamw_step(table: AdamWTable, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+def _device_number(name: str, v, dtype, table: AdamWTable):
+    """The address of a number on the device (None: it is one of the host's)."""
+    if not isinstance(v, torch.Tensor) or v.get_device() < 0:
+        return None
+    if v.dtype is not dtype or v.numel() != 1 or v.get_device() != table.table.get_device():
+        raise ValueError(f"{name} is a number of the host, or one of {dtype} on the device")
+    return v.data_ptr()
+
+
+def adamw_step(table: AdamWTable, step, lr, betas=(0.9, 0.999), eps: float = 1e-8,
                grad_scale=None, seed: int = 0, stream=None) -> None:
     """m3_adamw_step: one AdamW step (the `step`-th, from 1) over the table's tensors, in
     place.  `grad_scale` is a device scalar that every gradient is multiplied by (None:
-    1); `seed` feeds the 8-bit states' stochastic rounding: another for every step."""
+    1); `seed` feeds the 8-bit states' stochastic rounding: another for every step.
+
+    A captured step keeps `step`, `lr` and `seed`.  For one that goes on from replay to
+    replay give `step` as an int64 tensor of one element on the device, which the program
+    or the graph advances (the rounding's seed is then seed + step), and `lr`, where
+    it changes, as a float64 one."""
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                    or grad_scale.get_device() != table.table.get_device()):
         raise ValueError("grad_scale is one fp32 number on the device")
     if table.table.get_device() < 0:
         raise ValueError("libm3 takes tensors of a GPU")
-    c = M3AdamwConfig(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step),
-                      int(seed) & (2 ** 64 - 1))
+    at, rate = _device_number("step", step, torch.int64, table), _device_number("lr", lr, torch.float64, table)
+    c = M3AdamwConfig(0.0 if rate else float(lr), float(betas[0]), float(betas[1]), float(eps),
+                      0 if at else int(step), int(seed) & (2 ** 64 - 1), at, rate)
     _check(lib().m3_adamw_step(ctypes.byref(c), ctypes.byref(table.plan), table.table.data_ptr(),
                                None if grad_scale is None else grad_scale.data_ptr(), _stream(stream)))

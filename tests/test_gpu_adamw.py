@@ -274,3 +274,44 @@ def test_small_gradients_without_eps(eight, gtype):
             assert c.views("v")[k].float().gt(0).all()
         else:
             assert ((c.views("v")[k].double() - rv ** 2).abs() <= 4 * U * rv ** 2 + 1.5 * 2.0 ** -149).all(), k
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "8bit"])
+def test_captured_steps_go_on(eight):
+    """A step captured once with t and lr on the device: each replay is the next step,
+    with its bias corrections, its lr and its rounding, bit for bit the eager one."""
+    a, b = Case(12, eight, shapes=[(700,), (40, 30)]), Case(12, eight, shapes=[(700,), (40, 30)])
+    t = torch.ones(1, dtype=torch.int64, device=DEV)
+    lr = torch.full((1,), 0.5, dtype=torch.float64, device=DEV)
+    kw = dict(betas=(0.9, 0.95), eps=1e-8)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m3.adamw_step(b.table, step=t, lr=lr, seed=1000, **kw)
+        t.add_(1)
+    for k in range(1, 6):
+        rate = 1e-3 / k
+        lr.fill_(rate)
+        m3.adamw_step(a.table, step=k, lr=rate, seed=1000 + k, **kw)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert t.item() == k + 1
+        for name in a.flat:
+            assert torch.equal(a.flat[name].view(torch.uint8), b.flat[name].view(torch.uint8)), (k, name)
+        if eight:
+            assert all(torch.equal(x, y) for x, y in zip(a.scales, b.scales))
+    # not captured, with only one of the two on the device, and a t of no step
+    m3.adamw_step(a.table, step=6, lr=1e-4, seed=1006, **kw)
+    m3.adamw_step(b.table, step=t, lr=1e-4, seed=1000, **kw)
+    m3.adamw_step(a.table, step=7, lr=1e-3 / 5, seed=3, **kw)
+    m3.adamw_step(b.table, step=7, lr=lr, seed=3, **kw)
+    assert all(torch.equal(a.flat[name].view(torch.uint8), b.flat[name].view(torch.uint8)) for name in a.flat)
+    m3.adamw_step(a.table, step=8, lr=1e-4, seed=3, **kw)
+    m3.adamw_step(b.table, step=torch.tensor(8), lr=torch.tensor(1e-4, dtype=torch.float64), seed=3, **kw)   # (the host's)
+    assert all(torch.equal(a.flat[name].view(torch.uint8), b.flat[name].view(torch.uint8)) for name in a.flat)
+    for bad in (dict(step=t.int(), lr=1e-4), dict(step=t.repeat(2), lr=1e-4), dict(step=8, lr=lr.float())):
+        with pytest.raises(ValueError):
+            m3.adamw_step(b.table, **bad, **kw)
+    t.zero_()
+    m3.adamw_step(b.table, step=t, lr=1e-4, **kw)
+    assert all(torch.isnan(p).all() for p in b.views("p"))

@@ -303,3 +303,17 @@ def test_binding_refuses_workspaces_and_scalars_elsewhere():
     p = [torch.zeros(4, device="cuda")]
     with pytest.raises(ValueError):
         m3.adamw_step(m3.adamw_table(p, p, p, p), step=1, lr=1.0, grad_scale=torch.ones(1))
+
+
+def test_adamw_numbers_on_the_device(L):
+    """t and lr on the device: their alignment is checked, the host's are not looked at."""
+    _, p = plan(L, [tensor(n=0, p=None)])        # (nothing to do, nothing launched)
+
+    def step(device_step=None, device_lr=None, table=None, pl=p, **kw):
+        c = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, step=1, seed=0)
+        c.update(kw)
+        c = m3.M3AdamwConfig(*[c[k] for k in ("lr", "beta1", "beta2", "eps", "step", "seed")], device_step, device_lr)
+        return L.m3_adamw_step(ctypes.byref(c), ctypes.byref(pl), table, None, None)
+    assert step(device_step=FAKE + 4) == m3.M3_ERR_ALIGN and step(device_lr=FAKE + 4) == m3.M3_ERR_ALIGN
+    assert step(device_step=FAKE, step=0) == m3.M3_OK and step(device_lr=FAKE, step=0) == m3.M3_ERR_SHAPE
+    assert step(device_lr=FAKE, lr=float("nan")) == m3.M3_OK and step(device_step=FAKE, lr=float("nan")) == m3.M3_ERR_SHAPE
