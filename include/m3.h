@@ -571,13 +571,18 @@ m3_status m3_glr_check(const m3_glr_dims *dims, const void *workspace, size_t wo
  * in the io dtype.  Everything is overwritten.
  *
  * tokens 0 is allowed (the weight gradients are then zero; x, y, dy and dx may
- * be NULL).  Workspace: m3_ffn_workspace_bytes(dims, backward) bytes, no
- * initialisation (0 on invalid dims).  Rows that do not start on 16 bytes (odd
- * sizes or strides) are first copied there to rows that do.  Deterministic.
- * Alignment: the workspace 16 bytes; weights 16 bytes where their rows are
- * whole 16-byte pieces; else the element's (else M3_ERR_ALIGN).  dmodel and
+ * be NULL).  Workspace: m3_ffn_workspace_bytes(dims, what) bytes, no
+ * initialisation (0 on invalid dims), what = 0 or M3_FFN_BACKWARD.  Rows that do
+ * not start on 16 bytes (odd sizes or strides) are first copied there to rows
+ * that do.  Weights whose rows are whole 16-byte pieces but do not start on 16
+ * bytes (a view into a buffer of many tensors) are copied too, at every call,
+ * where the workspace has the bytes of M3_FFN_ANY_WEIGHTS (or'd to the others).
+ * Deterministic.  Alignment: the workspace 16 bytes; such weights, without that
+ * room, 16 bytes; everything else the element's (else M3_ERR_ALIGN).  dmodel and
  * dff are at most 2^16, the strides 2^20.  Outputs must not overlap inputs.
  */
+#define M3_FFN_BACKWARD 1
+#define M3_FFN_ANY_WEIGHTS 2
 #define M3_ACT_SILU 0
 #define M3_ACT_GELU 1
 typedef struct {
@@ -586,7 +591,7 @@ typedef struct {
     int32_t act;                    /* M3_ACT_*                               */
     int64_t x_stride, dy_stride;    /* elements between rows (dy_stride: backward) */
 } m3_ffn_dims;
-size_t m3_ffn_workspace_bytes(const m3_ffn_dims *dims, int backward);
+size_t m3_ffn_workspace_bytes(const m3_ffn_dims *dims, int what);
 m3_status m3_ffn_fwd(const m3_ffn_dims *dims, const void *x, const void *Wg, const void *Wu,
                      const void *Wd, void *y, void *workspace, size_t workspace_bytes, void *stream);
 m3_status m3_ffn_bwd(const m3_ffn_dims *dims, const void *x, const void *Wg, const void *Wu,

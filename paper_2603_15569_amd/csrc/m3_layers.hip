@@ -215,11 +215,12 @@ m3_status check_ffn(const m3_ffn_dims *d, bool bwd) {
 // Rows in the workspace start on 16 bytes: their lengths are whole pieces.
 struct FfnLayout {
     int64_t Dp, Fp;
-    bool pad_d, pad_f;             // weights with rows of dmodel, of dff, are copied
+    bool pad_d, pad_f;             // rows of dmodel, of dff, are no whole pieces
     int64_t some;                  // tokens the gates' backward takes at a time
     size_t x, dy, wg, wu, wd, h, dg, du, dh, part, total;
 };
-FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
+// any: room for copies of the weights wherever they start
+FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd, bool any) {
     const int64_t e = d->io == M3_F32 ? 4 : 2, el = 16 / e;
     FfnLayout w = {};
     w.Dp = (d->dmodel + el - 1) / el * el;
@@ -238,9 +239,9 @@ FfnLayout ffn_layout(const m3_ffn_dims *d, bool bwd) {
     };
     w.x = take(d->tokens, w.Dp, e);                       // (used where x's rows need it)
     w.dy = bwd ? take(d->tokens, w.Dp, e) : 0;
-    w.wg = take(w.pad_d ? d->dff : 0, w.Dp, e);
-    w.wu = take(w.pad_d ? d->dff : 0, w.Dp, e);
-    w.wd = take(w.pad_f ? d->dmodel : 0, w.Fp, e);
+    w.wg = take(w.pad_d || any ? d->dff : 0, w.Dp, e);
+    w.wu = take(w.pad_d || any ? d->dff : 0, w.Dp, e);
+    w.wd = take(w.pad_f || any ? d->dmodel : 0, w.Fp, e);
     w.h = take(d->tokens, w.Fp, e);
     w.dg = bwd ? take(d->tokens, w.Fp, e) : 0;
     w.du = bwd ? take(d->tokens, w.Fp, e) : 0;
@@ -290,18 +291,27 @@ struct Ffn {
 
 }  // namespace
 
-extern "C" size_t m3_ffn_workspace_bytes(const m3_ffn_dims *d, int backward) {
-    return check_ffn(d, backward != 0) == M3_OK ? ffn_layout(d, backward != 0).total : 0;
+extern "C" size_t m3_ffn_workspace_bytes(const m3_ffn_dims *d, int what) {
+    if (what & ~(M3_FFN_BACKWARD | M3_FFN_ANY_WEIGHTS)) return 0;
+    const bool bwd = (what & M3_FFN_BACKWARD) != 0;
+    return check_ffn(d, bwd) == M3_OK ? ffn_layout(d, bwd, (what & M3_FFN_ANY_WEIGHTS) != 0).total : 0;
 }
 
-static m3_status check_ffn_args(const m3_ffn_dims *d, const FfnLayout &w, const void *Wg, const void *Wu, const void *Wd,
-                                std::initializer_list<const void *> rest, const void *workspace, size_t workspace_bytes) {
+// The layout too: with room for copies where whole rows of weights need them
+static m3_status check_ffn_args(const m3_ffn_dims *d, bool bwd, const void *Wg, const void *Wu, const void *Wd,
+                                std::initializer_list<const void *> rest, const void *workspace, size_t workspace_bytes,
+                                FfnLayout *w) {
     if (!Wg || !Wu || !Wd) return M3_ERR_NULL;
     const uintptr_t e = d->io == M3_F32 ? 4 : 2;
-    if (!aligned(Wg, w.pad_d ? e : 16) || !aligned(Wu, w.pad_d ? e : 16) || !aligned(Wd, w.pad_f ? e : 16)) return M3_ERR_ALIGN;
+    for (const void *p : {Wg, Wu, Wd})
+        if (!aligned(p, e)) return M3_ERR_ALIGN;
     for (const void *p : rest)
         if (!aligned(p, e)) return M3_ERR_ALIGN;
-    if (!workspace || workspace_bytes < w.total) return M3_ERR_WORKSPACE;
+    *w = ffn_layout(d, bwd, false);
+    const bool any = (!w->pad_d && !(aligned(Wg, 16) && aligned(Wu, 16))) || (!w->pad_f && !aligned(Wd, 16));
+    if (any) *w = ffn_layout(d, bwd, true);
+    if (!workspace) return M3_ERR_WORKSPACE;
+    if (workspace_bytes < w->total) return any ? M3_ERR_ALIGN : M3_ERR_WORKSPACE;
     return aligned(workspace, 16) ? M3_OK : M3_ERR_ALIGN;
 }
 
@@ -309,9 +319,9 @@ extern "C" m3_status m3_ffn_fwd(const m3_ffn_dims *d, const void *x, const void 
                                 void *y, void *workspace, size_t workspace_bytes, void *stream) {
     m3_status s = check_ffn(d, false);
     if (s != M3_OK) return s;
-    const FfnLayout w = ffn_layout(d, false);
+    FfnLayout w;
     if (d->tokens > 0 && (!x || !y)) return M3_ERR_NULL;
-    s = check_ffn_args(d, w, Wg, Wu, Wd, {x, y}, workspace, workspace_bytes);
+    s = check_ffn_args(d, false, Wg, Wu, Wd, {x, y}, workspace, workspace_bytes, &w);
     if (s != M3_OK || d->tokens == 0) return s;
     const int64_t T = d->tokens, D = d->dmodel, F = d->dff;
     Ffn f{d, w, static_cast<char *>(workspace), static_cast<hipStream_t>(stream), d->io == M3_F32};
@@ -339,9 +349,9 @@ extern "C" m3_status m3_ffn_bwd(const m3_ffn_dims *d, const void *x, const void 
                                 size_t workspace_bytes, void *stream) {
     m3_status s = check_ffn(d, true);
     if (s != M3_OK) return s;
-    const FfnLayout w = ffn_layout(d, true);
+    FfnLayout w;
     if (!dWg || !dWu || !dWd || (d->tokens > 0 && (!x || !dy || !dx))) return M3_ERR_NULL;
-    s = check_ffn_args(d, w, Wg, Wu, Wd, {x, dy, dx, dWg, dWu, dWd}, workspace, workspace_bytes);
+    s = check_ffn_args(d, true, Wg, Wu, Wd, {x, dy, dx, dWg, dWu, dWd}, workspace, workspace_bytes, &w);
     if (s != M3_OK) return s;
     const int64_t T = d->tokens, D = d->dmodel, F = d->dff;
     Ffn f{d, w, static_cast<char *>(workspace), static_cast<hipStream_t>(stream), d->io == M3_F32};

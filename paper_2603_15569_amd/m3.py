@@ -806,12 +806,21 @@ def _ffn_dims(x, Wg, Wu, Wd, y, dy, act) -> M3FfnDims:
     return M3FfnDims(T, D, F, _IO[dtype], _ACT[act], *rows)
 
 
-def ffn_workspace(x, Wg, backward: bool = False) -> torch.Tensor:
+M3_FFN_BACKWARD, M3_FFN_ANY_WEIGHTS = 1, 2
+
+
+def ffn_workspace(x, Wg, backward: bool = False, any_weights: bool = False) -> torch.Tensor:
     """A workspace for ffn_fwd (ffn_bwd with `backward`, which serves both) of x
-    [..., D] and Wg [F, D]: keep it for further calls, one at a time."""
+    [..., D] and Wg [F, D]: keep it for further calls, one at a time.  `any_weights`: with
+    room for copies of weights that do not start on 16 bytes (made at every call)."""
     d = _ffn_dims(_meta(x), _meta(Wg), None, None, None, None, "silu")
-    n = int(lib().m3_ffn_workspace_bytes(ctypes.byref(d), int(backward)))
+    n = int(lib().m3_ffn_workspace_bytes(ctypes.byref(d), (M3_FFN_BACKWARD if backward else 0)
+                                         | (M3_FFN_ANY_WEIGHTS if any_weights else 0)))
     return torch.empty(max(n, 16), dtype=torch.uint8, device=x.device)
+
+
+def _off_16(*weights) -> bool:
+    return any(w.data_ptr() % 16 for w in weights)
 
 
 def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=None):
@@ -823,7 +832,7 @@ def ffn_fwd(x, Wg, Wu, Wd, act: str = "silu", out=None, workspace=None, stream=N
     d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), _meta(out), None, act)
     y = out if out is not None else _empty(x)
     if workspace is None:
-        workspace = ffn_workspace(x, Wg)
+        workspace = ffn_workspace(x, Wg, any_weights=_off_16(Wg, Wu, Wd))
     _check(lib().m3_ffn_fwd(ctypes.byref(d), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             y.data_ptr(), *_work(workspace, x), _stream(stream)))
     return y
@@ -837,7 +846,7 @@ def ffn_bwd(x, Wg, Wu, Wd, dy, act: str = "silu", workspace=None, stream=None):
     d = _ffn_dims(_meta(x), _meta(Wg), _meta(Wu), _meta(Wd), None, _meta(dy), act)
     out = dict(dx=_empty(x), dWg=_empty(Wg), dWu=_empty(Wu), dWd=_empty(Wd))
     if workspace is None:
-        workspace = ffn_workspace(x, Wg, backward=True)
+        workspace = ffn_workspace(x, Wg, backward=True, any_weights=_off_16(Wg, Wu, Wd))
     _check(lib().m3_ffn_bwd(ctypes.byref(d), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(),
                             dy.data_ptr(), out["dx"].data_ptr(), out["dWg"].data_ptr(), out["dWu"].data_ptr(),
                             out["dWd"].data_ptr(), *_work(workspace, x), _stream(stream)))

@@ -296,3 +296,31 @@ def test_given_stream_without_a_workspace():
         here.wait_stream(side)
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
         del busy
+
+
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,D,F", [(1, 64, 128), (9, 72, 40), (100, 128, 264), (300, 64, 100)])
+def test_weights_of_any_start(io, T, D, F):
+    """Weights as views that start on any element of a buffer, with the workspace left to
+    the call, or kept with room for them; without room they are refused."""
+    say(f"ffn any start {T} {D} {F} {io}")
+    x, Wg, Wu, Wd, dy = inputs(T, D, F, io, 31)
+    ref = reference(x, Wg, Wu, Wd, dy, "gelu", io)
+    buf = torch.full((3 * D * F + 30,), float("nan"), device=DEV, dtype=io)
+    views = []
+    for k, W in enumerate((Wg, Wu, Wd)):
+        at = k * (D * F + 9) + 1
+        views.append(buf[at:at + D * F].view(W.shape).copy_(W))
+    assert any(v.data_ptr() % 16 for v in views)
+    for weights in (views, [views[0], Wu, Wd], [Wg, Wu, views[2]]):
+        if not any(v.data_ptr() % 16 for v in weights):
+            continue
+        ws = m3.ffn_workspace(x, Wg, backward=True, any_weights=True)
+        for kw in ({}, dict(workspace=ws)):
+            check("y", m3.ffn_fwd(x, *weights, act="gelu", **kw), ref["y"])
+            for name, got in m3.ffn_bwd(x, *weights, dy, act="gelu", **kw).items():
+                check(name, got, ref[name])
+    es = 4 if io == torch.float32 else 2
+    if D * es % 16 == 0 and views[0].data_ptr() % 16:
+        with pytest.raises(m3.M3Error):
+            m3.ffn_fwd(x, *views, workspace=m3.ffn_workspace(x, Wg))

@@ -317,3 +317,21 @@ def test_adamw_numbers_on_the_device(L):
     assert step(device_step=FAKE + 4) == m3.M3_ERR_ALIGN and step(device_lr=FAKE + 4) == m3.M3_ERR_ALIGN
     assert step(device_step=FAKE, step=0) == m3.M3_OK and step(device_lr=FAKE, step=0) == m3.M3_ERR_SHAPE
     assert step(device_lr=FAKE, lr=float("nan")) == m3.M3_OK and step(device_step=FAKE, lr=float("nan")) == m3.M3_ERR_SHAPE
+
+
+def test_ffn_room_for_any_weights(L):
+    """Weights of whole rows that do not start on 16 bytes are refused where the workspace
+    has no room for their copies; the room asked for is that of the three."""
+    def call(d, weights, wsb):
+        return L.m3_ffn_fwd(ctypes.byref(d), None, *weights, None, FAKE, wsb, None)
+    d, none = ffn(), ffn(tokens=0)      # (no tokens: nothing to do, nothing launched)
+    size = lambda d, what: L.m3_ffn_workspace_bytes(ctypes.byref(d), what)  # noqa: E731
+    for what in (0, m3.M3_FFN_BACKWARD):
+        assert size(d, what | m3.M3_FFN_ANY_WEIGHTS) - size(d, what) == 3 * 64 * 160 * 2
+    assert size(d, 4) == 0
+    odd = ffn(dmodel=65, x_stride=65, dff=161)                       # (copied anyway)
+    assert size(odd, m3.M3_FFN_ANY_WEIGHTS) == size(odd, 0)
+    room = size(none, m3.M3_FFN_ANY_WEIGHTS)
+    for weights in ((FAKE + 2, FAKE, FAKE), (FAKE, FAKE + 8, FAKE), (FAKE, FAKE, FAKE + 14)):
+        assert call(none, weights, room - 1) == m3.M3_ERR_ALIGN and call(none, weights, room) == m3.M3_OK
+        assert call(none, [w + 1 for w in weights], room) == m3.M3_ERR_ALIGN
