@@ -16,10 +16,10 @@
 // reduction; more blocks a wave were slower (four: 5.9 TB/s).  132 small tensors
 // of 2.4 million elements in all: 13.5 us, 11 of them the bytes'.  Operations are
 // rounded to fp32 one by one.  The 8-bit step has enough of them to wait for
-// the vector units: with the library's root and quotients 857 us for 268
-// million parameters (bf16 gradients and copy), 783 (5.5 TB/s) with the
-// hardware's, the ones that the codes depend on refined; without the
-// refinement 717, but an ulp there turns codes over.
+// the vector units: 770 us for 268 million parameters (bf16 gradients and copy; 5.6
+// TB/s) with the hardware's root and reciprocal, the ones that the codes depend on
+// refined; a tenth more with the library's, a tenth less without the refinement,
+// but an ulp there turns codes over.
 #include "m3_adamw.h"
 #include "m3_device.h"
 
@@ -235,8 +235,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_adamw(Args a) {
     else block<G, kEight, false>(t, k, shrink, seed, base, left, lane);
 }
 
-// (one thread: the powers in fp64 for every wave would cost the 8-bit step its
-// spare time)
+// (one thread, 3 us before the step: the powers in fp64 for every wave would cost
+// the 8-bit step, which has no vector time to spare, more)
 __global__ void k_now(NowArgs a) {
     const int64_t t = a.device_step ? *a.device_step : a.step;
     const double lr = a.device_lr ? *a.device_lr : a.lr;

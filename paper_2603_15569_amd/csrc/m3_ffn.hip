@@ -13,14 +13,23 @@
 // where there are enough of them, 128 x 128 (four of 64 x 64, two workgroups a
 // unit) elsewhere; 128 and 64 in fp32.  The larger a wave's tile, the fewer bytes
 // of LDS a product: a step of the large one reads 192 KB and writes 64 KB for
-// 2048 cycles of the matrix units.  8192 tokens, 2048 -> 8192 in bf16: the gates
-// 401 us (1370 TFLOP/s), the way back 192 (1430), where a library's product of
-// this size reaches 1610; with everything on the card at work a step takes 1.54
-// us, with 32 units 1.1, so the clock and the operands' way through L2 bound it,
-// and next the epilogues, which nothing else hides (5 us a round of tiles, 22
-// in the backward, whose gates read dh and write three arrays).  fp32: the matrix
-// units, 140 TFLOP/s of the library's 154 (2048 tokens, 2048 -> 8192); small
-// products lose a third of it to the last round of tiles.
+// 2048 cycles of the matrix units.  8192 tokens, 2048 -> 8192 in bf16: 650 us, 442
+// the gates and 204 the way back (1240 and 1350 TFLOP/s; a library's products of
+// these sizes 1450 and 1580).  The matrix units are busy 57 and 62% of the cycles
+// (44% in the gates' backward) at a clock of 2.07 GHz, without LDS conflicts: the
+// clock, 2.4 with little at work, costs a seventh, and for two cycles of five
+// the units wait, for a stage's loads (all of them, once a step: a step takes 1.1
+// us with 32 compute units at work and 1.54 with all 256) and in the epilogues,
+// which nothing else hides (5 us a round of tiles, 22 in the backward, whose gates
+// read dh and write three arrays).  fp32: the matrix units, 140 TFLOP/s of the
+// library's 154 (2048 tokens, 2048 -> 8192); small products lose a third of it to
+// the last round of tiles.
+//
+// Roundings: sums, g, u, the activation and dh stay in fp32.  In bf16 h, dg and du
+// are rounded to bf16 once, as operands of the next product: the matrix units take
+// bf16 pairs, and keeping the cut-off part as a second operand would double
+// those products.  A result is then off by 0.0023 of its size (root mean square)
+// where its own rounding alone would leave 0.0017.
 //
 // Edges: buffer loads return zero past the end of an operand, so rows past M,
 // N or (turned) K need no masks; k past K within a row is sent out of range.
@@ -471,9 +480,9 @@ hipError_t join(const JoinArgs &g, int batch, bool f32, hipStream_t s) {
 // global memory (rows past the workgroup's out of range), x (read again by every
 // workgroup, from the caches) its columns, 16 a tile.  The waves' sums meet in LDS.
 // Without gates k may be split over workgroups too (the parts joined after).
-// Loading x a unit ahead as well cost more in registers than it gave (48 tokens:
-// 39.5 us a block, 41.8).  2048 -> 8192 in bf16: one token 12.5 us the gates (5.4
-// TB/s of weights), 9.0 the way back (3.7); 48 tokens 18 and 13.5.
+// Loading x a unit ahead as well cost more in registers than it gave (5% more time
+// at 48 tokens).  2048 -> 8192 in bf16: one token 12.1 us the gates (5.5 TB/s of
+// weights), 9.2 the way back (3.6); 48 tokens 18 and 13, and 4 to join.
 template <typename T, int TT, int RT, bool kGates>
 __global__ __launch_bounds__(512) void k_few(FewArgs a) {
     constexpr int NW = 8, NM = kGates ? 2 : 1, U = NM * RT * TT >= 8 ? 2 : 4;

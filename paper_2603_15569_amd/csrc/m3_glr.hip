@@ -18,8 +18,10 @@
 // Bound by HBM, and by the look-back where a sequence has few tiles: 16 tokens a
 // wave are what its registers hold with the gate (123 of them), so a compute unit
 // keeps 200 KB of loads on their way.  65536 tokens of 2048 channels in bf16:
-// forward 250 us (4.3 TB/s), backward 405 (4.6); 4 x 2048 of 4096 with the gate
-// and inputs as slices: 75 us (4.5).  3 x 1001 tokens of 1000 channels in fp32, one
+// forward 247 us (4.3 TB/s of the operator's bytes), backward 398 (4.7); 4 x 2048 of
+// 4096 with the gate and inputs as slices: 75 us (4.5).  A streaming kernel reaches
+// 6.1; 10 to 20% more bytes move than the operator has (the maps and states of
+// the look-back, and their polling).  3 x 1001 tokens of 1000 channels in fp32, one
 // and a half workgroups a unit: 18 us forward, 32 backward.
 #include <type_traits>
 
@@ -60,9 +62,9 @@ template <typename T> __device__ __forceinline__ Rows rows(const void *p, int64_
     return Rows{__builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(p) + at), (short)0, bytes, 0x00020000), st, n};
 }
 // Outputs go past the caches (kOnce): nothing here reads them again, and the
-// inputs keep the room (4 x 2048 of 4096 forward: 86 us, 77 so).  The
-// backward's loads too, the last use of its inputs (65536 x 2048: 430 us, 409
-// so); the forward's not (82 us), the backward reads them again.
+// inputs keep the room (a tenth of the time of 4 x 2048 of 4096 forward).  The
+// backward's loads too, the last use of its inputs (a twentieth of 65536 x 2048);
+// the forward's not (they cost it a sixteenth), the backward reads them again.
 // (W: the buffer is known to hold the row)
 constexpr int kOnce = 2;
 template <typename R, int kAux = 0, typename W> __device__ __forceinline__ R row_load(const Rows &w, int s, uint32_t off, W) {
@@ -174,11 +176,12 @@ struct Words {
 // The state that enters a tile (tile > 0, all threads of the workgroup).  Each
 // wave polls one of the NW tiles before this one; when that was not enough and
 // the sequence's start is in reach, kReach of them, back to `first`, the state
-// there (32 tiles of 512 channels: 13.9 us against 19.7 without; further into
-// a sequence the wider polling costs more than it saves, 261 us -> 284 at 512
-// tiles of 2048 channels).  The nearest tile whose state is known, with the
-// maps of all after it, gives the state, folded in token order.  `enter` is the
-// state of the lane's channels, NaN when the wait gave up.
+// there (4096 tokens of 512 channels: 13.8 us against 15.7 without; further into
+// a sequence the wider polling mostly costs more than it saves, 247 us -> 278 at
+// 65536 tokens of 2048 channels, 54 -> 59 at 2 x 16384 of 768, though not where
+// the channels are few, 72 -> 45 at 32768 of 256).  The nearest tile whose state is
+// known, with the maps of all after it, gives the state, folded in token order.
+// `enter` is the state of the lane's channels, NaN when the wait gave up.
 constexpr int kReach = 4;
 template <int V, int NW> struct Polled {
     float v[kReach * NW][2][64 * V];   // the state after the tile, or its map
